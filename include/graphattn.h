@@ -56,7 +56,26 @@ typedef enum {
   GA_EUNSUPPORTED = -5   /* head_dim, page_size or dtype outside what the kernels implement */
 } ga_status;
 
-typedef enum { GA_F32 = 0, GA_BF16 = 1 } ga_dtype;
+/* GA_MXFP4: the pool holds 4-bit values and q, k_new, v_new, k_out, v_out and out are bf16 (see
+ * "MXFP4 pools" below). */
+typedef enum { GA_F32 = 0, GA_BF16 = 1, GA_MXFP4 = 2 } ga_dtype;
+
+/* MXFP4 pools (a quarter of bf16's bytes: 4.25 bits a value).  Each block of 32 channels of one
+ * token's K or V shares a power of two: byte E, scale 2^(E - 127) (E = 255: every value of the block
+ * is NaN).  A value is a 4-bit code: bit 3 the sign, bits 0..2 one of 0, 0.5, 1, 1.5, 2, 3, 4, 6, times
+ * the block's scale.  Appending rounds a block with largest magnitude a to e = floor(log2 a) - 2, plus
+ * one where a >= 7 x 2^e, held in [-125, 125] (E = e + 127; a block of zeros has E = 2), and every
+ * value x to the code nearest to x / 2^e, ties to the even code; a block with a NaN or an infinity has
+ * E = 255.  Attention reads the values exactly as stored (they are bf16 numbers); nothing else differs
+ * from a bf16 pool.
+ *   kv_page_pool  [num_pages][Hkv][17 D] bytes, 16-byte aligned.  With t = 0..15 a page's token and c
+ *                 = 0..D-1 a channel (a byte holds an even channel's code in its low half, the next
+ *                 channel's in its high half), a kv-head's 17 D bytes are
+ *     K codes     8 D    token rows of D / 2 bytes
+ *     V codes     8 D    [t / 4][c / (D / 16)][t % 4][(c % (D / 16)) / 2]
+ *     K scales    D / 2  [t][c / 32]
+ *     V scales    D / 2  [t / 4][c / 32][t % 4]
+ * All entry points that take ga_params take this type. */
 
 /* The rollout graph's segments: one segment per generated step (edge) plus the prompt (root).
  * seg_len[s] >= 1 tokens; seg_page_offsets is CSR into seg_pages with seg_page_offsets[0] = 0,
@@ -85,7 +104,8 @@ typedef struct {
   int32_t head_dim;        /* D: 64 or 128 */
   int32_t page_size;       /* tokens per page: 16 */
   int64_t num_pages;       /* extent of kv_page_pool, for range checks */
-  int32_t dtype;           /* ga_dtype of q and kv_page_pool (and of out unless out_f32) */
+  int32_t dtype;           /* ga_dtype of q and kv_page_pool (and of out unless out_f32);
+                              GA_MXFP4: of the pool, the others are bf16 */
   float softmax_scale;     /* 0 selects 1/sqrt(head_dim) */
   int32_t out_f32;         /* 0: out has dtype; 1: out is float32 (no final rounding) */
 } ga_params;
@@ -258,7 +278,8 @@ ga_status graphattn_plan_profile_read(ga_plan* plan, ga_profile* out);
  * the tokens after the cut to fresh pages with this call.  Destinations must be distinct and
  * disjoint from the sources (otherwise the result is unspecified).
  *
- * Both: pool, k_new and v_new 16-byte aligned; num_tokens >= 0 (0: nothing is launched). */
+ * Both: pool, k_new and v_new 16-byte aligned; num_tokens >= 0 (0: nothing is launched).  For an MXFP4
+ * pool append rounds as stated at GA_MXFP4, and copy moves codes and scales. */
 ga_status graphattn_kv_append(void* kv_page_pool, const void* k_new, const void* v_new,
                               const int32_t* slot_words, int32_t num_tokens,
                               const ga_params* params, void* hip_stream);

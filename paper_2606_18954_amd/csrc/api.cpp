@@ -1,6 +1,6 @@
 // Host runtime of the graph-segment decode attention library: validation, plans, workspace,
 // launches and the C entry points declared in include/graphattn.h.
-#include "../../include/graphattn.h"
+#include "../../include/graphattn_cache.h"
 
 #include <algorithm>
 #include <cmath>
@@ -11,6 +11,7 @@
 #include <string>
 #include <vector>
 
+#include "evict_internal.hpp"
 #include "ga_internal.hpp"
 
 namespace {
@@ -115,7 +116,8 @@ struct ga_plan {
   // side rebuilds the chains' page lists from arrays uploaded with the graph (la).
   bool updatable = false;
   std::vector<int64_t> h_page_off;
-  std::vector<int32_t> h_pages;    // (kept until the first upload has packed it)
+  std::vector<int32_t> h_pages;
+  int distinct = -1;               // no page twice among the segments on a path (-1: not looked yet)
   std::vector<int32_t> h_last, h_counts;
   ga::LengthArgs la{};
   size_t len_off = 0;              // byte offset of the device copy of the lengths
@@ -156,7 +158,7 @@ ga_status validate_params(const ga_params* p) {
     return fail(GA_EUNSUPPORTED, "head_dim %d unsupported (64 or 128)", p->head_dim);
   if (p->page_size != ga::kPageTokens)
     return fail(GA_EUNSUPPORTED, "page_size %d unsupported (16)", p->page_size);
-  if (p->dtype != GA_F32 && p->dtype != GA_BF16)
+  if (p->dtype != GA_F32 && p->dtype != GA_BF16 && p->dtype != GA_MXFP4)
     return fail(GA_EUNSUPPORTED, "dtype %d unsupported", p->dtype);
   if (p->num_pages < 0) return fail(GA_EINVAL, "num_pages is negative");
   if (p->num_pages > (1LL << ga::kPageValidShift))
@@ -350,8 +352,9 @@ void size_schedule(const ga_segment_table* st, const ga_branch_paths* bp, const 
   // workgroup) 38.6 | 42.2, 32 queries 121 | 54; merged DAGs of 24 prompts, 2 queries (56 rows, 200
   // pages a workgroup) 249 | 245; 12/12 heads x 64, 8 queries (32 rows) 269.6 | 273.6.  One query per
   // branch stays on the other kernel, whose bits decode has.
+  const bool fp4 = p->dtype == GA_MXFP4;
   const bool many_rows =
-      multi_query && p->dtype == GA_BF16 &&
+      multi_query && (p->dtype == GA_BF16 || fp4) &&
       (row_pages >= 128 * ref_pages ||
        (row_pages >= 48 * ref_pages && block_pages * p->num_kv_heads >= 64 * wgs));
   const int64_t work = (many_rows ? block_pages : ref_pages) * p->num_kv_heads;
@@ -434,8 +437,8 @@ Layout layout(const Sizes& z, const ga_params& p) {
   sz[L_BPART_OFF] = sizeof(int64_t) * (z.B + 1);
   sz[L_BPART] = sizeof(int32_t) * z.prows;
   sz[L_BLK_SUM] = sizeof(int64_t) * ((z.E + 1023) / 1024 + 1);
-  // Partials: fp16 values + (lambda, scale) for bf16 inputs, fp32 values + lambda for fp32.
-  const bool f16_parts = p.dtype == GA_BF16;
+  // Partials: fp16 values + (lambda, scale) for bf16 queries, fp32 values + lambda for fp32.
+  const bool f16_parts = p.dtype != GA_F32;
   // (none where the attention kernel writes the rows itself)
   const size_t parts = z.direct ? 0 : (size_t)z.prows * p.num_q_heads;
   sz[L_PO] = (f16_parts ? 2 : 4) * parts * p.head_dim;
@@ -660,7 +663,8 @@ ga_status plan_init(const ga_segment_table* st, const ga_branch_paths* bp, const
   }
   size_schedule(&cst, &cbp, p, c.npg, npg_cap, pl->num_cus,
                 query_counts != nullptr, query_counts && pl->z.B > bp->num_branches, &pl->z);
-  pl->z.direct = query_counts && !pl->z.few_pages && !p->out_f32 && pl->z.prows == pl->z.B;
+  pl->z.direct = ((query_counts && !pl->z.few_pages) || p->dtype == GA_MXFP4) && !p->out_f32 &&
+                 pl->z.prows == pl->z.B;
   if (pl->z.prows > 0x7fffffffLL)
     return fail(GA_EINVAL, "too many partial rows (%lld)", (long long)pl->z.prows);
   if (pl->z.P > 0x7fffffffLL)
@@ -709,8 +713,6 @@ ga_status upload(ga_plan* pl, const Layout& L, bool pinned, hipStream_t stream) 
       std::memcpy(h + L.off[L_BR_COUNT], pl->h_counts.data(), sizeof(int32_t) * z.B0q);
     }
   }
-  pl->h_pages.clear();
-  pl->h_pages.shrink_to_fit();
   const size_t bytes = upload_bytes(L);
   if (pinned && bytes > 0 && bytes <= kKernelUploadBytes) {
     hipLaunchKernelGGL(k_upload, dim3((unsigned)((bytes + 16 * 256 - 1) / (16 * 256))), dim3(256), 0,
@@ -758,6 +760,13 @@ ga_status do_schedule(ga_plan* pl, hipStream_t stream) {
   return GA_OK;
 }
 
+// Attention workgroups of a plan's persistent grid on a device of num_cus CUs.
+int attn_grid(const ga_plan* pl, int num_cus) {
+  if (pl->p.dtype == GA_MXFP4) return num_cus * ga::kFp4WgsPerCu;
+  return ga::seg_attn_grid(pl->p.head_dim, pl->p.dtype == GA_BF16, pl->causal, pl->z.few_pages,
+                           num_cus);
+}
+
 ga_status do_run(ga_plan* pl, const void* q, const void* pool, void* out, float* lse,
                  hipStream_t stream) {
   ga_status rc = check_run_ptrs(pl, q, pool, out, lse);
@@ -772,7 +781,8 @@ ga_status do_run(ga_plan* pl, const void* q, const void* pool, void* out, float*
   // well.  If a launch below fails, the plan loses its schedule, so the next run schedules (and
   // so re-arms the heads) before it attends.
   pl->scheduled = false;
-  const bool bf16 = pl->p.dtype == GA_BF16;
+  const bool fp4 = pl->p.dtype == GA_MXFP4;
+  const bool bf16 = pl->p.dtype == GA_BF16 || fp4;   // type of q (and out)
   ga::AttnArgs a{};
   a.q = q;
   a.pool = pool;
@@ -787,12 +797,12 @@ ga_status do_run(ga_plan* pl, const void* q, const void* pool, void* out, float*
   a.desc_words = pl->z.desc_words;
   a.streams = ga::attn_streams(a.Hkv, pl->causal);
   a.scale_log2 = pl->p.softmax_scale * 1.4426950408889634f;
+  a.fp4 = fp4;
   if (pl->z.direct) {
     a.out = out;
     a.lse = lse;
   }
-  int64_t grid = (int64_t)ga::seg_attn_grid(pl->p.head_dim, bf16, pl->causal, pl->z.few_pages,
-                                            pl->num_cus);
+  int64_t grid = attn_grid(pl, pl->num_cus);
   const int64_t work = pl->z.max_items * pl->p.num_kv_heads;
   if (work < grid) grid = work;
   // Profiled runs bind their events to the attention and merge dispatches themselves (a kernel
@@ -844,6 +854,51 @@ void profile_clear(ga_plan* pl) {
 }
 
 }  // namespace
+
+namespace ga {
+
+ga_status plan_mass_args(ga_plan* plan, bool schedule, hipStream_t stream, MassArgs* a,
+                         int64_t* rows) {
+  *rows = plan->z.B;
+  if (plan->z.B == 0) return GA_OK;
+  if (plan->distinct < 0) {
+    // Two segments on paths that name the same page would both write its slots.  (All pages they
+    // own: later lengths may use them.)
+    int32_t top = -1;
+    for (const int32_t pg : plan->h_pages) top = std::max(top, pg);
+    std::vector<bool> seen((size_t)top + 1, false);
+    bool twice = false;
+    for (int32_t s = 0; s < plan->cg.S0; ++s)
+      if (plan->cg.vid[s] >= 0)
+        for (int64_t i = plan->h_page_off[s]; i < plan->h_page_off[s + 1]; ++i) {
+          twice = twice || seen[plan->h_pages[i]];
+          seen[plan->h_pages[i]] = true;
+        }
+    plan->distinct = twice ? 0 : 1;
+  }
+  if (!plan->distinct) return fail(GA_EINVAL, "two segments of the plan own the same page");
+  if (schedule && !plan->scheduled) {
+    const ga_status rc = do_schedule(plan, stream);
+    if (rc) return rc;
+  }
+  a->desc = plan->sc.desc;
+  a->counters = plan->sc.counters;
+  a->grp_br = plan->sc.grp_br;
+  a->desc_words = plan->z.desc_words;
+  a->chunk_pages = plan->z.chunk_pages;
+  a->Hq = plan->p.num_q_heads;
+  a->Hkv = plan->p.num_kv_heads;
+  a->group = a->Hq / a->Hkv;
+  a->head_dim = plan->p.head_dim;
+  a->dtype = plan->p.dtype;
+  a->causal = plan->causal;
+  a->scale_log2 = plan->p.softmax_scale * 1.4426950408889634f;
+  a->units = plan->z.max_items;
+  a->num_cus = plan->num_cus;
+  return GA_OK;
+}
+
+}  // namespace ga
 
 extern "C" {
 
@@ -994,8 +1049,7 @@ ga_status graphattn_plan_info(const ga_plan* plan, ga_plan_info* info) {
   info->rows_per_block = ga::kRowsPerBlock;
   info->num_items = -1;
   info->num_partial_rows = plan->z.prows;
-  info->workgroups_per_cu = ga::seg_attn_grid(plan->p.head_dim, plan->p.dtype == GA_BF16,
-                                              plan->causal, plan->z.few_pages, 1);
+  info->workgroups_per_cu = attn_grid(plan, 1);
   info->work_streams = ga::attn_streams(plan->p.num_kv_heads, plan->causal);
   if (plan->scheduled) {
     int64_t n = 0;
@@ -1265,17 +1319,18 @@ ga_status graphattn_decode_static(const void* q, const void* kv_page_pool,
 
 static ga_status kv_write(void* pool, const void* k_new, const void* v_new, const int32_t* src,
                           const int32_t* dst, int32_t n, const ga_params* params,
-                          void* hip_stream) {
+                          void* hip_stream, void* k_out = nullptr, void* v_out = nullptr) {
   g_err.clear();
   ga_status rc = validate_params(params);
   if (rc) return rc;
   if (n < 0) return fail(GA_EINVAL, "num_tokens is negative");
   if (n == 0) return GA_OK;
-  if (!pool || !dst || (src == nullptr && (!k_new || !v_new)))
+  if (!pool || !dst || (!src && !(k_new && v_new) && !(k_out && v_out)))
     return fail(GA_EINVAL, "device pointers must be non-NULL");
   if ((reinterpret_cast<uintptr_t>(pool) | reinterpret_cast<uintptr_t>(k_new) |
-       reinterpret_cast<uintptr_t>(v_new)) & 15)
-    return fail(GA_EINVAL, "kv_page_pool, k_new and v_new must be 16-byte aligned");
+       reinterpret_cast<uintptr_t>(v_new) | reinterpret_cast<uintptr_t>(k_out) |
+       reinterpret_cast<uintptr_t>(v_out)) & 15)
+    return fail(GA_EINVAL, "kv_page_pool and the K and V rows must be 16-byte aligned");
   if ((reinterpret_cast<uintptr_t>(dst) | reinterpret_cast<uintptr_t>(src)) & 3)
     return fail(GA_EINVAL, "slot word arrays must be 4-byte aligned");
   ga::KvWriteArgs a{};
@@ -1287,7 +1342,10 @@ static ga_status kv_write(void* pool, const void* k_new, const void* v_new, cons
   a.num_slots = params->num_pages * ga::kPageTokens;
   a.n = n;
   a.Hkv = params->num_kv_heads;
-  a.row_bytes = params->head_dim * (params->dtype == GA_BF16 ? 2 : 4);
+  a.row_bytes = params->head_dim * (params->dtype == GA_F32 ? 4 : 2);
+  a.k_out = static_cast<unsigned char*>(k_out);
+  a.v_out = static_cast<unsigned char*>(v_out);
+  a.fp4_dim = params->dtype == GA_MXFP4 ? params->head_dim : 0;
   if ((int64_t)n * a.Hkv * 2 * (a.row_bytes / 16) > 0x7fffffffLL * 256)
     return fail(GA_EINVAL, "too many tokens (%d)", n);
   GA_HIP(ga::launch_kv_write(a, static_cast<hipStream_t>(hip_stream)), "kv write launch");
@@ -1310,6 +1368,28 @@ ga_status graphattn_kv_copy(void* kv_page_pool, const int32_t* src_slot_words,
   }
   return kv_write(kv_page_pool, nullptr, nullptr, src_slot_words, dst_slot_words, num_tokens,
                   params, hip_stream);
+}
+
+ga_status graphattn_kv_read(const void* kv_page_pool, const int32_t* slot_words,
+                            int32_t num_tokens, void* k_out, void* v_out, const ga_params* params,
+                            void* hip_stream) {
+  if ((!k_out || !v_out) && num_tokens > 0) {
+    g_err.clear();
+    return fail(GA_EINVAL, "k_out or v_out is NULL");
+  }
+  return kv_write(const_cast<void*>(kv_page_pool), nullptr, nullptr, nullptr, slot_words,
+                  num_tokens, params, hip_stream, k_out, v_out);
+}
+
+int64_t graphattn_kv_page_bytes(const ga_params* params) {
+  g_err.clear();
+  const ga_status rc = validate_params(params);
+  if (rc) return rc;
+  const int64_t D = params->head_dim;
+  // K and V of 16 tokens of a kv-head: 32 D values, or 17 D bytes (mxfp4.hpp).
+  const int64_t head = params->dtype == GA_MXFP4 ? 17 * D
+                                                 : 32 * D * (params->dtype == GA_BF16 ? 2 : 4);
+  return head * params->num_kv_heads;
 }
 
 ga_status graphattn_extend(const void* q, const void* kv_page_pool,

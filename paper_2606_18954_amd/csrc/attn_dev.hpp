@@ -11,6 +11,9 @@ namespace ga {
 __host__ __device__ constexpr int mq_wgs_per_cu(int head_dim) { return head_dim == 64 ? 3 : 2; }
 hipError_t launch_mq_attn(const AttnArgs& a, int head_dim, int grid, hipStream_t stream,
                           hipEvent_t t0, hipEvent_t t1);
+// Attention over MXFP4 pools (fp4_attn.hip).
+hipError_t launch_fp4_attn(const AttnArgs& a, int head_dim, bool causal, int grid,
+                           hipStream_t stream, hipEvent_t t0, hipEvent_t t1);
 
 namespace {
 

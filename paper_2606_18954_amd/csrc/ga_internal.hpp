@@ -15,6 +15,8 @@ constexpr int kRowsPerBlock = 128;
 // Upper bound on pages per work item (the chunk's page ids are staged in LDS).
 constexpr int kMaxChunkPages = 128;
 constexpr int kAttnThreads = 256;        // 4 wave64 per workgroup
+// Attention workgroups per CU over an MXFP4 pool (fp4_attn.hip): two waves per SIMD, by registers.
+constexpr int kFp4WgsPerCu = 2;
 
 // Work-item descriptor (int32 words, one per item, fixed stride), written by the scheduler and
 // copied whole into LDS by the attention kernel:
@@ -112,8 +114,10 @@ struct AttnArgs {
   int32_t desc_words;      // descriptor stride (int32 words)
   int32_t streams;         // work streams: divides Hkv and kMaxStreams
   float scale_log2;        // softmax scale * log2(e)
+  bool fp4;                // pool holds MXFP4 pages (mxfp4.hpp); q and out are bf16
   // Multi-query launches whose rows all have one partial: the attention kernel writes them itself,
   // as bf16 (nullptr: partial rows, folded by the merge).
+  // (MXFP4 pools: decode launches as well.)
   void* out;
   float* lse;
 };
@@ -131,7 +135,8 @@ struct MergeArgs {
 
 // Page-pool writes (kv_write.hip): token j goes to slot word dst_words[j] (page * 16 + slot),
 // from k_new / v_new [n][Hkv][D] (append, src_words == nullptr) or from the pool slot
-// src_words[j] (copy).  Tokens whose words fall outside [0, num_slots) are skipped.
+// src_words[j] (copy).  With k_out / v_out, the tokens dst_words name are read out instead.  Tokens
+// whose words fall outside [0, num_slots) are skipped.
 struct KvWriteArgs {
   unsigned char* pool;
   const unsigned char* k_new;
@@ -140,6 +145,8 @@ struct KvWriteArgs {
   const int32_t* dst_words;
   int64_t num_slots;       // num_pages * 16
   int32_t n, Hkv, row_bytes;
+  unsigned char *k_out, *v_out;
+  int32_t fp4_dim;         // head_dim of an MXFP4 pool, else 0
 };
 
 // Equivalence detection (equiv.hip).  z [N][dim] bf16 bits; items: (first row state, first

@@ -17,7 +17,8 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libgraphattn.so")
 
 GA_OK, GA_EINVAL, GA_ERANGE, GA_ENOMEM, GA_EHIP, GA_EUNSUPPORTED = 0, -1, -2, -3, -4, -5
-GA_F32, GA_BF16 = 0, 1
+GA_F32, GA_BF16, GA_MXFP4 = 0, 1, 2
+DTYPES = {"f32": GA_F32, "bf16": GA_BF16, "mxfp4": GA_MXFP4}
 STATUS_NAMES = {0: "GA_OK", -1: "GA_EINVAL", -2: "GA_ERANGE", -3: "GA_ENOMEM", -4: "GA_EHIP",
                 -5: "GA_EUNSUPPORTED"}
 
@@ -103,6 +104,10 @@ def load_library() -> ctypes.CDLL:
     lib.graphattn_kv_append.restype = ctypes.c_int
     lib.graphattn_kv_copy.argtypes = [vp, vp, vp, i32, P(Params), vp]
     lib.graphattn_kv_copy.restype = ctypes.c_int
+    lib.graphattn_kv_read.argtypes = [vp, vp, i32, vp, vp, P(Params), vp]
+    lib.graphattn_kv_read.restype = ctypes.c_int
+    lib.graphattn_kv_page_bytes.argtypes = [P(Params)]
+    lib.graphattn_kv_page_bytes.restype = i64
     lib.graphattn_equivalence_classes.argtypes = [vp, i32, i32, P(StateForest), ctypes.c_float,
                                                   vp, vp]
     lib.graphattn_equivalence_classes.restype = ctypes.c_int
@@ -125,6 +130,14 @@ def load_library() -> ctypes.CDLL:
     lib.graphattn_plan_set_lengths.restype = ctypes.c_int
     lib.graphattn_run.argtypes = [vp, vp, vp, vp, vp, vp]
     lib.graphattn_run.restype = ctypes.c_int
+    lib.graphattn_run_mass.argtypes = [vp, vp, vp, vp, vp, ctypes.c_float, vp, vp]
+    lib.graphattn_run_mass.restype = ctypes.c_int
+    lib.graphattn_evict_create.argtypes = [P(SegmentTable), P(i32), i32, i32, i64, vp, P(vp)]
+    lib.graphattn_evict_create.restype = ctypes.c_int
+    lib.graphattn_evict_select.argtypes = [vp, vp, vp, vp, vp]
+    lib.graphattn_evict_select.restype = ctypes.c_int
+    lib.graphattn_evict_destroy.argtypes = [vp]
+    lib.graphattn_evict_destroy.restype = None
     lib.graphattn_plan_info.argtypes = [vp, P(PlanInfo)]
     lib.graphattn_plan_info.restype = ctypes.c_int
     lib.graphattn_plan_debug_dump.argtypes = [vp, vp, P(i64), P(i32), P(i32), P(i32), P(i32),
@@ -175,7 +188,7 @@ class HostGraph:
 def make_params(num_q_heads: int, num_kv_heads: int, head_dim: int, num_pages: int, dtype: str,
                 softmax_scale: float = 0.0, out_f32: bool = False) -> Params:
     return Params(num_q_heads, num_kv_heads, head_dim, 16, num_pages,
-                  GA_BF16 if dtype == "bf16" else GA_F32, softmax_scale, int(bool(out_f32)))
+                  DTYPES.get(dtype, GA_F32), softmax_scale, int(bool(out_f32)))
 
 
 def _stream_handle(stream) -> int:
@@ -265,6 +278,45 @@ def kv_copy(pool, src_words, dst_words, params: Params, stream=None):
         raise ValueError("one source word per destination word")
     _check(lib.graphattn_kv_copy(_dev_ptr(pool), _dev_ptr(src_words), _dev_ptr(dst_words), n,
                                  ctypes.byref(params), _stream_handle(stream)))
+
+
+def kv_read(pool, slot_words, params: Params, k_out=None, v_out=None, stream=None):
+    """graphattn_kv_read: the K and V of the tokens at slot_words, (k [n, Hkv, D], v [n, Hkv, D]);
+    rows of words outside the pool are left as they were (zero where this call allocates)."""
+    import torch
+    lib = load_library()
+    n = int(slot_words.numel())
+    shape = (n, params.num_kv_heads, params.head_dim)
+    dt = torch.float32 if params.dtype == GA_F32 else torch.bfloat16
+    if k_out is None:
+        k_out = torch.zeros(shape, dtype=dt, device=pool.device)
+    if v_out is None:
+        v_out = torch.zeros(shape, dtype=dt, device=pool.device)
+    if tuple(k_out.shape) != shape or tuple(v_out.shape) != shape:
+        raise ValueError("one K row and one V row [Hkv, D] per slot word")
+    _check(lib.graphattn_kv_read(_dev_ptr(pool), _dev_ptr(slot_words), n, _dev_ptr(k_out),
+                                 _dev_ptr(v_out), ctypes.byref(params), _stream_handle(stream)))
+    return k_out, v_out
+
+
+def kv_page_bytes(params: Params) -> int:
+    """graphattn_kv_page_bytes: bytes of one page of the pool, all kv-heads."""
+    n = int(load_library().graphattn_kv_page_bytes(ctypes.byref(params)))
+    if n < 0:
+        _check(n)
+    return n
+
+
+def empty_pool(params: Params, device="cuda"):
+    """An uninitialised pool for these parameters: [num_pages, Hkv, 2, 16, D], or for MXFP4 pages
+    uint8 [num_pages, Hkv, 17 D]."""
+    import torch
+    kv_page_bytes(params)
+    n, h, d = params.num_pages, params.num_kv_heads, params.head_dim
+    if params.dtype == GA_MXFP4:
+        return torch.empty((n, h, 17 * d), dtype=torch.uint8, device=device)
+    dt = torch.float32 if params.dtype == GA_F32 else torch.bfloat16
+    return torch.empty((n, h, 2, 16, d), dtype=dt, device=device)
 
 
 class HostForest:
@@ -425,6 +477,17 @@ class Plan:
         _check(self.lib.graphattn_run(self.handle, _dev_ptr(q), _dev_ptr(pool), _dev_ptr(out),
                                       _dev_ptr(lse), _stream_handle(stream)))
 
+    def run_mass(self, q, pool, lse, mass_out, mass_in=None, decay: float = 1.0, stream=None):
+        """graphattn_run_mass: the attention weight every cached token received from these rows
+        (lse as run() wrote it), added to decay x mass_in (float32 [num_pages x 16])."""
+        for t in (mass_out, mass_in):
+            if t is not None and t.numel() < 16 * self.params.num_pages:
+                raise ValueError("one mass per slot of the pool")
+        _check(self.lib.graphattn_run_mass(self.handle, _dev_ptr(q), _dev_ptr(pool), _dev_ptr(lse),
+                                           _dev_ptr(mass_in), float(decay), _dev_ptr(mass_out),
+                                           _stream_handle(stream)))
+        return mass_out
+
     def info(self) -> PlanInfo:
         inf = PlanInfo()
         _check(self.lib.graphattn_plan_info(self.handle, ctypes.byref(inf)))
@@ -478,6 +541,66 @@ class Plan:
             pass
 
 
+class Evict:
+    """graphattn_evict_create / select / destroy: the tokens of every segment that stay.
+
+    offsets [S + 1] (host int64): where each segment's tokens start in the selection's outputs."""
+
+    def __init__(self, graph: HostGraph, keep_counts, first: int, recent: int, num_pages: int,
+                 stream=None):
+        self.handle = None
+        self.lib = load_library()
+        keep = np.ascontiguousarray(keep_counts, dtype=np.int32)
+        if len(keep) != graph.st.num_segments:
+            raise ValueError("one keep count per segment")
+        self.offsets = np.concatenate([[0], np.cumsum(keep, dtype=np.int64)])
+        self.num_pages = int(num_pages)
+        h = ctypes.c_void_p()
+        _check(self.lib.graphattn_evict_create(ctypes.byref(graph.st), _ptr(keep, ctypes.c_int32),
+                                               int(first), int(recent), int(num_pages),
+                                               _stream_handle(stream), ctypes.byref(h)))
+        self.handle = h
+
+    @property
+    def total(self) -> int:
+        """Tokens that stay, over all segments."""
+        return int(self.offsets[-1])
+
+    def select(self, mass, positions=None, slot_words=None, stream=None):
+        """(positions, slot_words), int32 [total] each, from the mass of every slot."""
+        import torch
+        if mass.numel() < 16 * self.num_pages:
+            raise ValueError("one mass per slot of the pool")
+        if positions is None:
+            positions = torch.empty(self.total, dtype=torch.int32, device=mass.device)
+        if slot_words is None:
+            slot_words = torch.empty(self.total, dtype=torch.int32, device=mass.device)
+        if positions.numel() < self.total or slot_words.numel() < self.total:
+            raise ValueError("one position and one slot word per token that stays")
+        if self.total:
+            _check(self.lib.graphattn_evict_select(self.handle, _dev_ptr(mass),
+                                                   _dev_ptr(positions), _dev_ptr(slot_words),
+                                                   _stream_handle(stream)))
+        return positions, slot_words
+
+    def close(self):
+        if self.handle:
+            self.lib.graphattn_evict_destroy(self.handle)
+            self.handle = None
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
 def validate_only(graph: HostGraph, params: Params, query_counts=None) -> int:
     """Run the library's host-side validation through graphattn_decode (graphattn_extend with
     query_counts) with NULL device buffers; used by CPU tests of the error paths.  Returns the
@@ -496,10 +619,10 @@ def last_error() -> str:
     return load_library().graphattn_last_error().decode(errors="replace")
 
 
-def header_symbols() -> list:
-    """Function names declared in include/graphattn.h."""
+def header_symbols(header: str = "graphattn.h") -> list:
+    """Function names declared in include/graphattn.h (or another header there)."""
     import re
-    hdr = os.path.join(os.path.dirname(_PKG), "include", "graphattn.h")
+    hdr = os.path.join(os.path.dirname(_PKG), "include", header)
     text = open(hdr).read()
     text = re.sub(r"/\*.*?\*/", "", text, flags=re.S)
     return sorted(set(re.findall(r"\b(graphattn_\w+)\s*\(", text)))
