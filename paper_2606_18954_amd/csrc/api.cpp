@@ -894,7 +894,11 @@ ga_status plan_mass_args(ga_plan* plan, bool schedule, hipStream_t stream, MassA
   a->causal = plan->causal;
   a->scale_log2 = plan->p.softmax_scale * 1.4426950408889634f;
   a->units = plan->z.max_items;
-  a->num_cus = plan->num_cus;
+  // Pages a workgroup takes: its rows' queries are loaded once for them, but every CU wants several.
+  int64_t pages = 0;
+  for (const int32_t n : plan->cg.npg) pages += n;
+  a->pages = ga::kMassPages;
+  while (a->pages > 4 && pages < (int64_t)a->pages * 8 * plan->num_cus) a->pages /= 2;
   return GA_OK;
 }
 

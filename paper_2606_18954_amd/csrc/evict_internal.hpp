@@ -23,8 +23,9 @@ struct MassArgs {
   bool causal;             // a multi-query plan
   float scale_log2, decay;
   int64_t units;           // upper bound on items
-  int num_cus;
+  int32_t pages;           // pages a workgroup takes (at most kMassPages)
 };
+constexpr int32_t kMassPages = 32;
 hipError_t launch_mass(const MassArgs& a, hipStream_t stream);
 
 // The schedule and sizes of a plan as the mass kernel needs them (api.cpp); rows: query rows.

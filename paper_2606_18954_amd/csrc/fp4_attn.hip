@@ -27,6 +27,7 @@
 #include "attn_dev.hpp"
 #include "ga_internal.hpp"
 #include "mxfp4.hpp"
+#include "pool_load.hpp"
 
 #include <hip/hip_ext.h>
 
@@ -37,7 +38,6 @@ namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
 template <int D>
 struct QCfg {
@@ -47,7 +47,7 @@ struct QCfg {
   static constexpr int PF = 3;                      // pairs of pages in flight or in use per wave
 };
 
-// One page as loaded: K and V codes, K's scale byte, V's four.
+// One page as loaded: K and V codes, the word with K's scale, V's four scales.
 template <int D>
 struct Page {
   unsigned k[QCfg<D>::LW], v[QCfg<D>::LW];
@@ -55,13 +55,15 @@ struct Page {
 };
 
 template <int D>
-__device__ __forceinline__ void load_words(unsigned (&w)[QCfg<D>::LW], const unsigned char* p) {
+__device__ __forceinline__ void load_words(unsigned (&w)[QCfg<D>::LW], page_t page, unsigned off) {
   if constexpr (D == 128) {
-    const uint4 x = *reinterpret_cast<const uint4*>(p);
-    w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
+    const u32x4 x = load16(page, off);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = x[i];
   } else {
-    const uint2 x = *reinterpret_cast<const uint2*>(p);
-    w[0] = x.x; w[1] = x.y;
+    const u32x2 x = load8(page, off);
+    w[0] = x[0];
+    w[1] = x[1];
   }
 }
 
@@ -125,10 +127,12 @@ __global__ __launch_bounds__(kAttnThreads, kFp4WgsPerCu) void k_fp4_attn(AttnArg
   __syncthreads();
 
   const int64_t blk_stride = (int64_t)a.Hkv * F::PAGE;
-  const int k_off = r16 * (D / 2) + kg * (D / 8);
-  const int v_off = F::V + lane * (D / 8);
-  const int ks_off = F::KS + r16 * F::NS + (kg * (D / 4)) / 32;
-  const int vs_off = F::VS + (kg * F::NS + (r16 * F::SL) / 32) * 4;
+  // The lane's bytes of a page.
+  const unsigned k_off = r16 * (D / 2) + kg * (D / 8);
+  const unsigned v_off = F::V + lane * (D / 8);
+  const unsigned ks_byte = r16 * F::NS + (kg * (D / 4)) / 32;
+  const unsigned ks_off = F::KS + (ks_byte & ~3u), ks_shift = 8 * (ks_byte & 3);
+  const unsigned vs_off = F::VS + (kg * F::NS + (r16 * F::SL) / 32) * 4;
 
   bool first = true;
   for (int b = 0;; b ^= 1) {
@@ -165,13 +169,13 @@ __global__ __launch_bounds__(kAttnThreads, kFp4WgsPerCu) void k_fp4_attn(AttnArg
     auto run_unit = [&](auto nt_tag) {
       constexpr int NT = decltype(nt_tag)::value;
       auto load_page = [&](Page<D>& pg, int word) {
-        const unsigned char* base = pool_h + (int64_t)(word & kPageIdMask) * blk_stride;
-        load_words<D>(pg.k, base + k_off);
-        load_words<D>(pg.v, base + v_off);
-        pg.ks = base[ks_off];
-        pg.vs = *reinterpret_cast<const unsigned*>(base + vs_off);
+        const page_t page = page_at(pool_h + (int64_t)(word & kPageIdMask) * blk_stride, F::PAGE);
+        load_words<D>(pg.k, page, k_off);
+        load_words<D>(pg.v, page, v_off);
+        pg.ks = load4(page, ks_off);
+        pg.vs = load4(page, vs_off);
       };
-      const int last_pair = npairs - 1;
+      const int last_pair = max(npairs - 1, 0);
       auto load_pair = [&](Page<D> (&pp)[2], int p) {
         const int x = min(p, last_pair);
         load_page(pp[0], __builtin_amdgcn_readlane(pk0, x));
@@ -190,10 +194,8 @@ __global__ __launch_bounds__(kAttnThreads, kFp4WgsPerCu) void k_fp4_attn(AttnArg
 #pragma unroll
         for (int n = 0; n < C::NB; ++n) O[t][n] = f32x4{0.f, 0.f, 0.f, 0.f};
       }
-      if (npairs > 0) {
-#pragma unroll
-        for (int i = 0; i < C::PF; ++i) load_pair(buf[i], split + ks * i);
-      }
+      int claim = 0;
+      if (!first && wave == 0 && lane == 0) claim = atomicAdd(&heads[cs], 1);
       // Q operand: lane holds row r16 of the tile, channels kg D / 4 + 8 s ..+ 7 at step s.
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
@@ -214,18 +216,21 @@ __global__ __launch_bounds__(kAttnThreads, kFp4WgsPerCu) void k_fp4_attn(AttnArg
         // The lane's row sees chunk token 16 p + 4 kg + i only for 16 p + i <= cl.
         cl[t] = cm ? cw + (row0 + r) / a.group - 4 * kg : 0x3fffffff;
       }
-      // The next unit: claimed and fetched while this one streams.
+      // (The pages come behind the claim and the queries, whose waits then leave them in flight; they are
+      // loaded whether or not they exist, the last pair again, so that every path has the same loads
+      // outstanding.)
+#pragma unroll
+      for (int i = 0; i < C::PF; ++i) load_pair(buf[i], split + ks * i);
+      // The next unit's descriptor is fetched while this one streams.
       if (wave == 0) {
         int v;
         if (first) {
           v = unit_of(rank + gs(cs), cs);
         } else {
-          int c = 0;
-          if (lane == 0) c = atomicAdd(&heads[cs], 1);
-          int j = 2 * gs(cs) + __builtin_amdgcn_readfirstlane(c);
+          int j = 2 * gs(cs) + __builtin_amdgcn_readfirstlane(claim);
           for (int t = 1; j >= n_str && t < ns; ++t) {
             cs = cs + 1 == ns ? 0 : cs + 1;
-            c = 0;
+            int c = 0;
             if (lane == 0) c = atomicAdd(&heads[cs], 1);
             j = 2 * gs(cs) + __builtin_amdgcn_readfirstlane(c);
           }
@@ -233,7 +238,6 @@ __global__ __launch_bounds__(kAttnThreads, kFp4WgsPerCu) void k_fp4_attn(AttnArg
         }
         fetch_desc(v, b ^ 1);
       }
-
       auto pair = [&](Page<D> (&pp)[2], int p) {
         f32x4 S[2][NT];
         int valid[2];
@@ -251,7 +255,7 @@ __global__ __launch_bounds__(kAttnThreads, kFp4WgsPerCu) void k_fp4_attn(AttnArg
           }
 #pragma unroll
           for (int t = 0; t < NT; ++t) S[g][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-          const float sk = fp4_exp<0>(pp[g].ks);
+          const float sk = fp4_exp_at(pp[g].ks, ks_shift);
 #pragma unroll
           for (int s = 0; s < C::QS; ++s) {
             u32x4 ka;
@@ -356,10 +360,9 @@ __global__ __launch_bounds__(kAttnThreads, kFp4WgsPerCu) void k_fp4_attn(AttnArg
 #pragma unroll
         for (int i = 0; i < C::PF; ++i) {
           const int x = p + ks * i;
-          if (x < npairs) {
-            pair(buf[i], x);
-            load_pair(buf[i], x + C::PF * ks);
-          }
+          __builtin_amdgcn_sched_barrier(0);         // (nothing of a pair is touched before its turn)
+          if (x < npairs) pair(buf[i], x);
+          load_pair(buf[i], x + C::PF * ks);
         }
       }
 

@@ -58,5 +58,12 @@ __device__ __forceinline__ float fp4_exp(unsigned w) {
   return __builtin_bit_cast(float, (J < 3 ? w << (23 - 8 * J) : w >> 1) & 0x7f800000u);
 }
 
+// Byte at bit `shift` of w, as the float32 whose exponent it is.  (A wave reads scales as whole words: a
+// byte load's register is extended in place, which the compiler waits for where the value is moved.)
+__device__ __forceinline__ float fp4_exp_at(unsigned w, unsigned shift) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_ubfe(w, shift, 8) << 23);
+}
+
+
 }  // namespace
 }  // namespace ga
