@@ -117,6 +117,8 @@ struct ga_plan {
   bool updatable = false;
   std::vector<int64_t> h_page_off;
   std::vector<int32_t> h_pages;
+  int32_t mass_cost = 0, mass_parts = 0;    // how the attention mass takes the chains (0: not looked yet)
+  bool mass_many = false;
   int distinct = -1;               // no page twice among the segments on a path (-1: not looked yet)
   std::vector<int32_t> h_last, h_counts;
   ga::LengthArgs la{};
@@ -881,11 +883,12 @@ ga_status plan_mass_args(ga_plan* plan, bool schedule, hipStream_t stream, MassA
     const ga_status rc = do_schedule(plan, stream);
     if (rc) return rc;
   }
-  a->desc = plan->sc.desc;
-  a->counters = plan->sc.counters;
+  a->seg_len = plan->g.seg_len;
+  a->seg_page_off = plan->g.seg_page_off;
+  a->seg_pages = plan->g.seg_pages;
+  a->seg_causal = plan->g.seg_causal;
+  a->grp_off = plan->sc.grp_off;
   a->grp_br = plan->sc.grp_br;
-  a->desc_words = plan->z.desc_words;
-  a->chunk_pages = plan->z.chunk_pages;
   a->Hq = plan->p.num_q_heads;
   a->Hkv = plan->p.num_kv_heads;
   a->group = a->Hq / a->Hkv;
@@ -893,12 +896,28 @@ ga_status plan_mass_args(ga_plan* plan, bool schedule, hipStream_t stream, MassA
   a->dtype = plan->p.dtype;
   a->causal = plan->causal;
   a->scale_log2 = plan->p.softmax_scale * 1.4426950408889634f;
-  a->units = plan->z.max_items;
-  // Pages a workgroup takes: its rows' queries are loaded once for them, but every CU wants several.
-  int64_t pages = 0;
-  for (const int32_t n : plan->cg.npg) pages += n;
-  a->pages = ga::kMassPages;
-  while (a->pages > 4 && pages < (int64_t)a->pages * 8 * plan->num_cus) a->pages /= 2;
+  if (!plan->mass_cost) {
+    // What a workgroup takes: as much as leaves every CU several workgroups.
+    const CGraph& c = plan->cg;
+    std::vector<int64_t> rows(plan->z.S, 0);
+    for (const int32_t v : c.path_segs) rows[v] += plan->p.num_q_heads / plan->p.num_kv_heads;
+    int32_t cost = ga::kMassCost;
+    for (;; cost /= 2) {
+      int64_t parts = 0;
+      for (int32_t v = 0; v < plan->z.S; ++v) parts += ga::mass_parts(c.npg[v], rows[v], cost);
+      if (cost <= 4 || parts >= 12LL * plan->num_cus) break;
+    }
+    // (all pages a chain owns: later lengths may use them)
+    for (int32_t v = 0; v < plan->z.S; ++v)
+      plan->mass_parts = std::max(plan->mass_parts,
+                                  ga::mass_parts(c.seg_page_off[v + 1] - c.seg_page_off[v], rows[v], cost));
+    for (const int64_t r : rows) plan->mass_many = plan->mass_many || r > ga::kMassRows;
+    plan->mass_cost = cost;
+  }
+  a->chains = plan->z.S;
+  a->cost = plan->mass_cost;
+  a->many = plan->mass_many;
+  a->parts = plan->mass_parts;
   return GA_OK;
 }
 

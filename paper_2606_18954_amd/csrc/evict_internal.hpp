@@ -15,17 +15,31 @@ struct MassArgs {
   const float* lse;        // [R][Hq]
   const float* mass_in;    // [num_slots] or nullptr
   float* mass_out;         // [num_slots]
-  const int32_t* desc;     // the schedule: work-item descriptors, items, B(s)
-  const int64_t* counters;
+  const int32_t* seg_len;  // the plan's chains: tokens, page lists, causal origins, and their rows B(s)
+  const int64_t* seg_page_off;
+  const int32_t* seg_pages;
+  const int32_t* seg_causal;
+  const int64_t* grp_off;
   const int32_t* grp_br;
-  int32_t desc_words, chunk_pages;
   int32_t Hq, Hkv, group, head_dim, dtype;
   bool causal;             // a multi-query plan
   float scale_log2, decay;
-  int64_t units;           // upper bound on items
-  int32_t pages;           // pages a workgroup takes (at most kMassPages)
+  int32_t chains, parts;   // chains, and the most parts one of them may have
+  int32_t cost;            // what a workgroup takes: pages x pairs of row tiles
+  bool many;               // some chain has more than kMassRows rows
 };
-constexpr int32_t kMassPages = 32;
+// Rows of a chain that are taken two tiles at a time.
+constexpr int32_t kMassRows = 128;
+constexpr int32_t kMassCost = 128;     // most of it, and so most pages
+// Parts a chain is taken in: of about `cost` pages x pairs of row tiles, and of kMassPages pages at least.
+constexpr int32_t kMassPages = 4;
+__host__ __device__ inline int32_t mass_parts(int64_t pages, int64_t rows, int32_t cost) {
+  // (cost: a power of two, at most kMassCost)
+  const int64_t pairs = (rows + 31) / 32 < cost ? (rows + 31) / 32 : cost;
+  const int32_t parts = (int32_t)((pages * pairs + cost - 1) >> __builtin_ctz(cost));
+  const int32_t most = (int32_t)((pages + kMassPages - 1) / kMassPages);
+  return parts < most ? parts : most;
+}
 hipError_t launch_mass(const MassArgs& a, hipStream_t stream);
 
 // The schedule and sizes of a plan as the mass kernel needs them (api.cpp); rows: query rows.

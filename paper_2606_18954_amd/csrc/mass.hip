@@ -10,7 +10,7 @@
 // A lane holds four rows' scores of one token, so a token's sum is three additions in the lane; the
 // four lanes of a token meet in LDS, with the kv-heads, once per unit.
 //
-// Few rows (up to kFewTiles tiles: every page of a decode step): two tiles' queries stay in registers and
+// Few rows (up to kMassRows, most chains of a decode step): two tiles' queries stay in registers and
 // the pages stream past, several of them on their way, once per two tiles (from the caches after the first
 // time).  More rows (prefill): a few pages stay, as matrix operands, and the rows stream past, one tile's
 // queries and the next one's row numbers on their way.
@@ -28,7 +28,9 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 // Waves per SIMD the registers are kept to.
-constexpr int mass_waves(int D, int type) { return type == GA_F32 ? 2 : D == 64 ? 4 : 3; }
+constexpr int mass_waves(int D, int type, bool many) {
+  return type == GA_F32 ? (D == 64 ? 4 : 2) : !many || D == 64 ? 4 : 3;
+}
 
 template <int D, int TYPE>
 struct MCfg {
@@ -41,9 +43,6 @@ struct MCfg {
   // Pages on their way or in use (few rows).
   static constexpr int PF = TYPE == GA_MXFP4 ? 4 : NW <= 8 ? 3 : NW <= 16 ? 2 : 1;
 };
-
-// Most row tiles that are taken two at a time: a row block, whose branches the descriptor lists.
-constexpr int kFewTiles = kRowsPerBlock / 16;
 
 template <bool F32> struct Op;
 template <> struct Op<true> { float v; };
@@ -131,19 +130,29 @@ __device__ __forceinline__ float offset_of(float lse, bool live) {
                                                      : -__builtin_huge_valf();
 }
 
-template <int D, int TYPE, bool CAUSAL>
-__global__ __launch_bounds__(256, mass_waves(D, TYPE)) void k_mass(MassArgs a) {
+// MANY: some chain has more than kMassRows rows.  (The other variant has a third fewer registers, and so
+// more waves to hide the loads of a workgroup's start.)
+template <int D, int TYPE, bool CAUSAL, bool MANY>
+__global__ __launch_bounds__(256, mass_waves(D, TYPE, MANY)) void k_mass(MassArgs a) {
   using C = MCfg<D, TYPE>;
   using OpT = Op<C::F32>;
-  __shared__ float s_mass[4][kMassPages * 64];      // [kv-head slot][page][kg][token]
-  const int gpc = (a.chunk_pages + a.pages - 1) / a.pages;
-  const int item = (int)blockIdx.x / gpc;
-  const int pg0 = ((int)blockIdx.x - item * gpc) * a.pages;
-  if (item >= a.counters[0]) return;
-  const int32_t* d = a.desc + (int64_t)item * a.desc_words;
-  const int np = d[0], cw = d[1], cnt = d[3], goff = d[5];
-  if (d[4] != 0 || pg0 >= np) return;               // (the first row block's item takes all rows)
-  const int npg = min(a.pages, np - pg0);
+  extern __shared__ float s_mass[];                 // [kv-head slot][page][token]
+  // (part by part: those that most chains do not have come last)
+  const int part = (int)blockIdx.x / a.chains;
+  const int v = (int)blockIdx.x - part * a.chains;
+  const int np_all = (a.seg_len[v] + kPageTokens - 1) / kPageTokens;
+  const int64_t page0 = a.seg_page_off[v], goff = a.grp_off[v];
+  const int cnt = (int)(a.grp_off[v + 1] - goff);
+  const int cw = CAUSAL ? a.seg_causal[v] : kNoCausal;
+  const int rows = cnt * a.group;
+  const int nparts = mass_parts(np_all, rows, a.cost);    // equal ones
+  if (part >= nparts) return;
+  const int per = (np_all + nparts - 1) / nparts;
+  const int pg0 = part * per;
+  const int npg = min(per, np_all - pg0);
+  if (npg <= 0) return;
+  const int32_t* words = a.seg_pages + page0 + pg0;
+  const int32_t* branches = a.grp_br + goff;
   const int tid = threadIdx.x;
   const int lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -152,9 +161,8 @@ __global__ __launch_bounds__(256, mass_waves(D, TYPE)) void k_mass(MassArgs a) {
   const int rs = 4 / hs;                                  // waves that share a head's pages
   const int hslot = wave % hs, split = wave / hs;
   const unsigned char* q = static_cast<const unsigned char*>(a.q);
-  const int pw = d[kDescHead + pg0 + min(lane, npg - 1)]; // lane p: word of page pg0 + p
+  const int pw0 = words[min(lane, npg - 1)], pw1 = words[min(64 + lane, npg - 1)];   // a lane per page
   const bool cm = CAUSAL && cw != kNoCausal;
-  const int rows = cnt * a.group;
   const int ntile = (rows + 15) >> 4;
   const unsigned magic = 0xffffffffu / (unsigned)a.group;
   // r / group and its remainder: the truncated reciprocal is at most one short.
@@ -163,8 +171,8 @@ __global__ __launch_bounds__(256, mass_waves(D, TYPE)) void k_mass(MassArgs a) {
     gi = r - j * a.group;
     if (gi >= a.group) { gi -= a.group; ++j; }
   };
-  float* region = s_mass[hslot];
-  // The first tile with a row that sees page pg0 (causal units; the newest row sees every page).
+  float* region = s_mass + hslot * a.cost * kPageTokens;
+  // The first tile with a row that sees the page (a newest segment: its last row sees every page).
   auto first_tile = [&](int page) {
     return cm ? (int)(((int64_t)max(0, kPageTokens * page - cw) * a.group) >> 4) : 0;
   };
@@ -174,35 +182,40 @@ __global__ __launch_bounds__(256, mass_waves(D, TYPE)) void k_mass(MassArgs a) {
   for (int h = hslot; h < a.Hkv; h += hs) {
     const unsigned char* pool_h = static_cast<const unsigned char*>(a.pool) + (int64_t)h * C::HEAD;
     auto page_of = [&](int p) {
-      const int word = __builtin_amdgcn_readlane(pw, min(p, npg - 1));
+      const int x = min(p, npg - 1);
+      const int word = x < 64 ? __builtin_amdgcn_readlane(pw0, x) : __builtin_amdgcn_readlane(pw1, x - 64);
       return page_at(pool_h + (int64_t)(word & kPageIdMask) * a.Hkv * C::HEAD, C::HEAD);
     };
     auto put = [&](int p, float x, bool fresh) {
-      float* at = region + p * 64 + lane;
-      *at = fresh ? x : *at + x;
+      // the four lanes of a token
+      const auto h2 = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, x),
+                                                       __builtin_bit_cast(unsigned, x), false, false);
+      const unsigned lo = h2[0], hi = h2[1];
+      x = __builtin_bit_cast(float, lo) + __builtin_bit_cast(float, hi);
+      const auto q2 = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, x),
+                                                       __builtin_bit_cast(unsigned, x), false, false);
+      const unsigned lo2 = q2[0], hi2 = q2[1];
+      x = __builtin_bit_cast(float, lo2) + __builtin_bit_cast(float, hi2);
+      if (lane < kPageTokens) {
+        float* at = region + p * kPageTokens + lane;
+        *at = fresh ? x : *at + x;
+      }
     };
     // (A slot past the segment's end may hold anything: only its own sums see it, and they are not
     // stored.)
     auto few = [&](auto nt_tag, int t0) {
       constexpr int NT = decltype(nt_tag)::value;
       OpT qo[NT][C::OPS];
-      float nl[NT][4];
-      int lim[NT][4];
+      float lse[NT], nl[NT][4];
+      int rank[NT], lim[NT][4];
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         int j, gi;
         split_row(min(16 * (t0 + t) + r16, rows - 1), j, gi);
-        const int64_t row = (int64_t)d[kDescHead + a.chunk_pages + j] * a.Hq + h * a.group + gi;
+        const int64_t row = (int64_t)branches[j] * a.Hq + h * a.group + gi;
         load_row<D, C::F32>(qo[t], q + row * D * C::ELT, kg);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int r = 16 * (t0 + t) + 4 * kg + i;
-          split_row(min(r, rows - 1), j, gi);
-          const int64_t lr = (int64_t)d[kDescHead + a.chunk_pages + j] * a.Hq + h * a.group + gi;
-          nl[t][i] = offset_of(a.lse[lr], r < rows);
-          if constexpr (CAUSAL)
-            lim[t][i] = cw + j - kPageTokens * pg0 - r16;   // sees page p's token r16 for 16 p <= lim
-        }
+        lse[t] = a.lse[row];
+        rank[t] = j;
       }
       // (Behind the queries, whose wait then leaves the pages in flight.  The pages are loaded whether
       // or not they exist, the last one again, so that every path has the same loads outstanding, and
@@ -210,6 +223,17 @@ __global__ __launch_bounds__(256, mass_waves(D, TYPE)) void k_mass(MassArgs a) {
       RawK<D, TYPE> buf[C::PF];
 #pragma unroll
       for (int i = 0; i < C::PF; ++i) load_k<D, TYPE>(buf[i], page_of(split + rs * i), r16, kg);
+      // The lane's scores are of rows 4 kg + i of a tile.
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const float nr = offset_of(lse[t], 16 * (t0 + t) + r16 < rows);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          nl[t][i] = __shfl(nr, 4 * kg + i);
+          if constexpr (CAUSAL)                         // sees page p's token r16 for 16 p <= lim
+            lim[t][i] = cw + __shfl(rank[t], 4 * kg + i) - kPageTokens * pg0 - r16;
+        }
+      }
       for (int p0 = split; p0 < npg; p0 += rs * C::PF) {
 #pragma unroll
         for (int i = 0; i < C::PF; ++i) {
@@ -265,7 +289,7 @@ __global__ __launch_bounds__(256, mass_waves(D, TYPE)) void k_mass(MassArgs a) {
         auto row_of = [&](int x, int& j) {
           int gi;
           split_row(min(16 * x + r16, rows - 1), j, gi);
-          return (int64_t)a.grp_br[goff + j] * a.Hq + h * a.group + gi;
+          return (int64_t)branches[j] * a.Hq + h * a.group + gi;
         };
         OpT qo[C::OPS], qn[C::OPS];
         int j0 = 0, j1 = 0;
@@ -317,41 +341,62 @@ __global__ __launch_bounds__(256, mass_waves(D, TYPE)) void k_mass(MassArgs a) {
           if (p0 + g < npg) put(p0 + g, acc[g], h == hslot);
       }
     };
-    if (ntile > kFewTiles) {
-      many();
+    if (MANY && rows > kMassRows) {
+      if constexpr (MANY) many();
     } else {
       int t = tile0;
       for (; t + 1 < ntile; t += 2) few(std::integral_constant<int, 2>{}, t);
       if (t < ntile) few(std::integral_constant<int, 1>{}, t);
     }
   }
+  // The slots' earlier mass is on its way while the last waves come in.
+  constexpr int IN = kMassCost / 16;
+  float in[IN];
+  int64_t slot[IN];
+#pragma unroll
+  for (int i = 0; i < IN; ++i) {
+    const int p = i * 16 + (tid >> 4), tok = tid & 15;
+    slot[i] = -1;
+    in[i] = 0.f;
+    if (i * 16 < npg && p < npg) {
+      const int word = words[p];
+      if (tok <= (int)((unsigned)word >> kPageValidShift)) {
+        slot[i] = (int64_t)(word & kPageIdMask) * kPageTokens + tok;
+        if (a.mass_in) in[i] = a.mass_in[slot[i]];
+      }
+    }
+  }
   __syncthreads();
-  for (int x = tid; x < 16 * npg; x += 256) {
-    const int p = x >> 4, tok = x & 15;
-    const int word = d[kDescHead + pg0 + p];
-    if (tok > (int)((unsigned)word >> kPageValidShift)) continue;
+#pragma unroll
+  for (int i = 0; i < IN; ++i) {
+    if (slot[i] < 0) continue;
+    const int p = i * 16 + (tid >> 4), tok = tid & 15;
     float sum = 0.f;
     for (int k = 0; k < hs; ++k) {
-      const float* r = s_mass[k] + p * 64 + tok;
-      sum += (r[0] + r[16]) + (r[32] + r[48]);
+      sum += s_mass[(k * a.cost + p) * kPageTokens + tok];
     }
-    const int64_t slot = (int64_t)(word & kPageIdMask) * kPageTokens + tok;
-    a.mass_out[slot] = a.mass_in ? fmaf(a.decay, a.mass_in[slot], sum) : sum;
+    a.mass_out[slot[i]] = a.mass_in ? fmaf(a.decay, in[i], sum) : sum;
   }
 }
 
 template <int D>
 hipError_t launch_t(const MassArgs& a, hipStream_t stream) {
-  const int64_t grid = a.units * ((a.chunk_pages + a.pages - 1) / a.pages);
+  const int64_t grid = (int64_t)a.chains * a.parts;
   if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
+  const unsigned lds = 4 * a.cost * kPageTokens * sizeof(float);
   auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), lds, stream, a);
   };
   auto type = [&](auto causal) {
     constexpr bool CAUSAL = decltype(causal)::value;
-    if (a.dtype == GA_F32) go(k_mass<D, GA_F32, CAUSAL>);
-    else if (a.dtype == GA_BF16) go(k_mass<D, GA_BF16, CAUSAL>);
-    else go(k_mass<D, GA_MXFP4, CAUSAL>);
+    auto rows = [&](auto many) {
+      constexpr bool MANY = decltype(many)::value;
+      if (a.dtype == GA_F32) go(k_mass<D, GA_F32, CAUSAL, MANY>);
+      else if (a.dtype == GA_BF16) go(k_mass<D, GA_BF16, CAUSAL, MANY>);
+      else go(k_mass<D, GA_MXFP4, CAUSAL, MANY>);
+    };
+    if (a.many) rows(std::true_type{});
+    else rows(std::false_type{});
   };
   if (a.causal) type(std::true_type{});
   else type(std::false_type{});
@@ -361,7 +406,7 @@ hipError_t launch_t(const MassArgs& a, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_mass(const MassArgs& a, hipStream_t stream) {
-  if (a.units == 0) return hipSuccess;
+  if (a.chains == 0 || a.parts == 0) return hipSuccess;
   if (a.head_dim == 64) return launch_t<64>(a, stream);
   if (a.head_dim == 128) return launch_t<128>(a, stream);
   return hipErrorInvalidValue;
