@@ -81,6 +81,7 @@ struct Sizes {
   int32_t chunk_pages = 0;
   bool few_pages = false;      // decode: under 64 pages (x kv-heads) per workgroup at two per CU;
                                // multi-query: few query rows per page (size_schedule)
+  bool few_rows = false;       // MXFP4 pools: few query rows per page
   bool direct = false;         // every query row has one partial: no merge (multi-query plans)
   int64_t max_items = 0;       // upper bound on work items per kv-head
   int32_t desc_words = 0;      // work-item descriptor stride (int32 words)
@@ -370,6 +371,7 @@ void size_schedule(const ga_segment_table* st, const ga_branch_paths* bp, const 
   // A step this small gives each workgroup one or two units, whose fixed costs (first pages'
   // latency, partial stores) three workgroups per CU overlap better than two (bf16 decode).
   z->few_pages = causal ? !many_rows : work < 64 * wgs;
+  z->few_rows = fp4 && row_pages < 32 * ref_pages;
   int64_t chunks_ref = 0, prows = 0;
   for (int32_t s = 0; s < z->S; ++s)
     if (used[s]) chunks_ref += (npg_cap[s] + cap - 1) / cap;
@@ -764,7 +766,7 @@ ga_status do_schedule(ga_plan* pl, hipStream_t stream) {
 
 // Attention workgroups of a plan's persistent grid on a device of num_cus CUs.
 int attn_grid(const ga_plan* pl, int num_cus) {
-  if (pl->p.dtype == GA_MXFP4) return num_cus * ga::kFp4WgsPerCu;
+  if (pl->p.dtype == GA_MXFP4) return num_cus * ga::fp4_wgs_per_cu(pl->z.few_rows);
   return ga::seg_attn_grid(pl->p.head_dim, pl->p.dtype == GA_BF16, pl->causal, pl->z.few_pages,
                            num_cus);
 }
@@ -800,6 +802,7 @@ ga_status do_run(ga_plan* pl, const void* q, const void* pool, void* out, float*
   a.streams = ga::attn_streams(a.Hkv, pl->causal);
   a.scale_log2 = pl->p.softmax_scale * 1.4426950408889634f;
   a.fp4 = fp4;
+  a.few_rows = pl->z.few_rows;
   if (pl->z.direct) {
     a.out = out;
     a.lse = lse;

@@ -44,7 +44,6 @@ struct QCfg {
   static constexpr int LW = D / 32;                 // 32-bit words of K (or V) a lane holds per page
   static constexpr int QS = D / 32;                 // contraction steps of S^T = K Q^T
   static constexpr int NB = D / 16;                 // 16-column tiles of O^T
-  static constexpr int PF = 3;                      // pairs of pages in flight or in use per wave
 };
 
 // One page as loaded: K and V codes, the word with K's scale, V's four scales.
@@ -76,10 +75,12 @@ __device__ __forceinline__ float quad_sum(float v) {
   return v + __shfl_xor(v, 32);
 }
 
-template <int D, bool CAUSAL>
-__global__ __launch_bounds__(kAttnThreads, kFp4WgsPerCu) void k_fp4_attn(AttnArgs a) {
+// MAXNT: row tiles of a wave, one (steps with few rows a page) or two.
+template <int D, bool CAUSAL, int MAXNT>
+__global__ __launch_bounds__(kAttnThreads, fp4_wgs_per_cu(MAXNT == 1)) void k_fp4_attn(AttnArgs a) {
   using C = QCfg<D>;
   using F = Fp4<D>;
+  constexpr int PF = MAXNT == 1 ? 2 : 3;            // pairs of pages in flight or in use per wave
   __shared__ __align__(1024) int s_desc[2][kDescMaxBytes / 4];
   __shared__ __align__(16) float s_o[4][16 * D];    // a row tile of each wave, chunks XOR-permuted
   __shared__ float s_m[4][16], s_l[4][16];
@@ -153,21 +154,22 @@ __global__ __launch_bounds__(kAttnThreads, kFp4WgsPerCu) void k_fp4_attn(AttnArg
     int np = np0;
     if (cm) np = max(0, min(np0, (cw + (row0 + R - 1) / a.group + kPageTokens) / kPageTokens));
     const int npairs = (np + 1) >> 1;
-    const unsigned char* pool_h = (const unsigned char*)uniform64(
-        (int64_t)(uintptr_t)(pool + (int64_t)kvh * F::PAGE));
-
-    // ks waves share the pages of a tile group; ng tile groups, group tg holds tiles tg + ng t.
-    const int ks = nrt <= 2 ? 4 : nrt <= 4 ? 2 : 1;
-    const int ng = 4 / ks;
-    const int tg = wave % ng, split = wave / ng;
-
     // Words of the pair's pages, a lane per pair (the second page of a last pair may not exist: the
     // first once more, masked).
     const int pk0 = dsc[kDescHead + max(0, min(2 * lane, np - 1))];
     const int pk1 = dsc[kDescHead + max(0, min(2 * lane + 1, np - 1))];
 
-    auto run_unit = [&](auto nt_tag) {
+    const unsigned char* pool_h = (const unsigned char*)uniform64(
+        (int64_t)(uintptr_t)(pool + (int64_t)kvh * F::PAGE));
+
+    // One pass over the pages: ng groups of ks = 4 / ng waves.  The waves of a group share row tiles
+    // (group g: tiles tile0 + g + ng t) and take pairs of pages in turn.
+    auto run_pass = [&](auto nt_tag, int ng, int tile0) {
       constexpr int NT = decltype(nt_tag)::value;
+      const int ks = 4 / ng;
+      const int grp = wave % ng, split = wave / ng;
+      const bool claims = tile0 == 0;                // (the unit's first pass)
+      auto tile_of = [&](int g, int t) { return tile0 + g + ng * t; };
       auto load_page = [&](Page<D>& pg, int word) {
         const page_t page = page_at(pool_h + (int64_t)(word & kPageIdMask) * blk_stride, F::PAGE);
         load_words<D>(pg.k, page, k_off);
@@ -182,7 +184,7 @@ __global__ __launch_bounds__(kAttnThreads, kFp4WgsPerCu) void k_fp4_attn(AttnArg
         load_page(pp[1], __builtin_amdgcn_readlane(pk1, x));
       };
 
-      Page<D> buf[C::PF][2];
+      Page<D> buf[PF][2];
       bf16x8 qop[NT][C::QS];
       float m[NT], l[NT];
       f32x4 O[NT][C::NB];
@@ -195,11 +197,11 @@ __global__ __launch_bounds__(kAttnThreads, kFp4WgsPerCu) void k_fp4_attn(AttnArg
         for (int n = 0; n < C::NB; ++n) O[t][n] = f32x4{0.f, 0.f, 0.f, 0.f};
       }
       int claim = 0;
-      if (!first && wave == 0 && lane == 0) claim = atomicAdd(&heads[cs], 1);
+      if (claims && !first && wave == 0 && lane == 0) claim = atomicAdd(&heads[cs], 1);
       // Q operand: lane holds row r16 of the tile, channels kg D / 4 + 8 s ..+ 7 at step s.
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        const int r = (tg + ng * t) * 16 + r16;
+        const int r = tile_of(grp, t) * 16 + r16;
         const bool live = r < R;
         const __bf16* qp = qbase;
         if (live) {
@@ -220,9 +222,9 @@ __global__ __launch_bounds__(kAttnThreads, kFp4WgsPerCu) void k_fp4_attn(AttnArg
       // loaded whether or not they exist, the last pair again, so that every path has the same loads
       // outstanding.)
 #pragma unroll
-      for (int i = 0; i < C::PF; ++i) load_pair(buf[i], split + ks * i);
+      for (int i = 0; i < PF; ++i) load_pair(buf[i], split + ks * i);
       // The next unit's descriptor is fetched while this one streams.
-      if (wave == 0) {
+      if (claims && wave == 0) {
         int v;
         if (first) {
           v = unit_of(rank + gs(cs), cs);
@@ -356,25 +358,97 @@ __global__ __launch_bounds__(kAttnThreads, kFp4WgsPerCu) void k_fp4_attn(AttnArg
           vtiles(std::integral_constant<int, 3>{});
         }
       };
-      for (int p = split; p < npairs; p += C::PF * ks) {
+      for (int p = split; p < npairs; p += PF * ks) {
 #pragma unroll
-        for (int i = 0; i < C::PF; ++i) {
+        for (int i = 0; i < PF; ++i) {
           const int x = p + ks * i;
           __builtin_amdgcn_sched_barrier(0);         // (nothing of a pair is touched before its turn)
           if (x < npairs) pair(buf[i], x);
-          load_pair(buf[i], x + C::PF * ks);
+          load_pair(buf[i], x + PF * ks);
         }
       }
 
-      // End of the unit: tile t of every wave goes to LDS, and the threads join the splits' parts
-      // and write the rows, D / 8 threads a row.
+      // End of the pass.
       if (wave == 0) wait_vmcnt(0);                  // (the next descriptor)
       int lane_e = lane;
       asm volatile("" : "+v"(lane_e));
       const int re = lane_e & 15, ke = lane_e >> 4;
-      const int nrounds = (nrt + ng - 1) / ng;
+      if (ks == 1) {
+        // A wave that saw every page writes its rows itself: D / 4 consecutive columns a lane, column
+        // e D / 16 + n of them in O[n][e].
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
+        for (int t = 0; t < NT; ++t) {
+          const int r = tile_of(grp, t) * 16 + re;
+          const float L = quad_sum(l[t]);
+          const float inv = L > 0.f ? 1.f / L : 0.f;
+          const float lam = m[t] + log2_(L);
+          float amax = 0.f;
+          if (!a.out) {
+#pragma unroll
+            for (int n = 0; n < C::NB; ++n)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) amax = fmaxf(amax, fabsf(O[t][n][e]));
+            amax = quad_max(amax) * inv;
+          }
+          if (r < R) {
+            const int gr = row0 + r;
+            const int j = gr / a.group;
+            const int h = kvh * a.group + (gr - j * a.group);
+            if (a.out) {
+              const int64_t orow = (int64_t)dsc[br_word + j - j0] * a.Hq + h;
+              __bf16* dst = static_cast<__bf16*>(a.out) + orow * D + ke * (D / 4);
+#pragma unroll
+              for (int x = 0; x < D / 32; ++x) {
+                bf16x8 v;
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                  v[i] = (__bf16)(O[t][(8 * x + i) % C::NB][(8 * x + i) / C::NB] * inv);
+                *reinterpret_cast<bf16x8*>(dst + 8 * x) = v;
+              }
+              if (ke == 0) a.lse[orow] = lam * 0.69314718055994531f;
+            } else {
+              const int64_t prow = ((int64_t)prow_base + j) * a.Hq + h;
+              const int e = max(__builtin_amdgcn_frexp_expf(amax), -100);
+              const float up = __builtin_amdgcn_ldexpf(inv, kPartScaleBits - e);
+              _Float16* dst = static_cast<_Float16*>(a.po) + prow * D;
+              if constexpr (D == 128) {
+                // Position 32 ke + 16 (x / 2) + 8 (x % 2) ..: columns 8 (x / 2) + 4 (x % 2) ..+ 3 of the
+                // lane's, then those 16 further.
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                  f16x8 v;
+#pragma unroll
+                  for (int i = 0; i < 4; ++i) {
+                    v[i] = (_Float16)(O[t][4 * (x & 1) + i][x >> 1] * up);
+                    v[4 + i] = (_Float16)(O[t][4 * (x & 1) + i][(x >> 1) + 2] * up);
+                  }
+                  store_dev16(reinterpret_cast<f16x8*>(dst + 32 * ke + 8 * x), v);
+                }
+              } else {
+                // Position 32 (ke / 2) + 8 x + 4 (ke % 2) ..: columns 4 x ..+ 3 of the lane's.
+                typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                  f16x4 v;
+#pragma unroll
+                  for (int i = 0; i < 4; ++i) v[i] = (_Float16)(O[t][i][x] * up);
+                  store_dev8(reinterpret_cast<f32x2*>(dst + 32 * (ke >> 1) + 8 * x + 4 * (ke & 1)),
+                             __builtin_bit_cast(f32x2, v));
+                }
+              }
+              if (ke == 0)
+                store_dev8(reinterpret_cast<f32x2*>(a.plse + 2 * prow),
+                           f32x2{lam, __builtin_amdgcn_ldexpf(1.f, e - kPartScaleBits)});
+            }
+          }
+        }
+        return;
+      }
+      // Otherwise tile t of every wave goes to LDS, and the threads join the splits' parts and write the
+      // rows, D / 8 threads a row.
+      const int nrounds = min(MAXNT, (nrt - tile0 + ng - 1) / ng);
+#pragma unroll
+      for (int t = 0; t < MAXNT; ++t) {
         if (t >= nrounds) break;
         lds_barrier();                               // the round before is read
         if (t < NT) {
@@ -403,7 +477,7 @@ __global__ __launch_bounds__(kAttnThreads, kFp4WgsPerCu) void k_fp4_attn(AttnArg
         const int tasks = ng * 16 * TPR;
         for (int x = tid; x < tasks; x += kAttnThreads) {
           const int row = (x / TPR) & 15, gq = x / (16 * TPR), pc = x % TPR;
-          const int r = (gq + ng * t) * 16 + row;
+          const int r = tile_of(gq, t) * 16 + row;
           if (r < R) {                               // (the threads of a row go together)
             float M = NEG_INF;
             for (int s = 0; s < ks; ++s) M = fmaxf(M, s_m[gq + ng * s][row]);
@@ -463,8 +537,16 @@ __global__ __launch_bounds__(kAttnThreads, kFp4WgsPerCu) void k_fp4_attn(AttnArg
         }
       }
     };
-    if (tg + ng < nrt) run_unit(std::integral_constant<int, 2>{});
-    else run_unit(std::integral_constant<int, 1>{});
+    const std::integral_constant<int, 1> one{};
+    if constexpr (MAXNT == 1) {
+      const int ng = nrt <= 2 ? nrt : 4;
+      for (int t0 = 0; t0 < nrt; t0 += ng)
+        if (t0 + wave % ng < nrt) run_pass(one, ng, t0);
+    } else {
+      const int ng = nrt <= 2 ? 1 : nrt <= 4 ? 2 : 4;
+      if (wave % ng + ng < nrt) run_pass(std::integral_constant<int, 2>{}, ng, 0);
+      else run_pass(one, ng, 0);
+    }
     first = false;
     lds_barrier();        // the rows are read from LDS, and nothing needs this unit's descriptor
   }
@@ -488,8 +570,13 @@ hipError_t launch_t(const AttnArgs& a, bool causal, int grid, hipStream_t stream
     else
       hipLaunchKernelGGL(kernel, dim3(grid), dim3(kAttnThreads), 0, stream, a);
   };
-  if (causal) go(k_fp4_attn<D, true>);
-  else go(k_fp4_attn<D, false>);
+  if (a.few_rows) {
+    if (causal) go(k_fp4_attn<D, true, 1>);
+    else go(k_fp4_attn<D, false, 1>);
+  } else {
+    if (causal) go(k_fp4_attn<D, true, 2>);
+    else go(k_fp4_attn<D, false, 2>);
+  }
   return hipGetLastError();
 }
 

@@ -15,8 +15,8 @@ constexpr int kRowsPerBlock = 128;
 // Upper bound on pages per work item (the chunk's page ids are staged in LDS).
 constexpr int kMaxChunkPages = 128;
 constexpr int kAttnThreads = 256;        // 4 wave64 per workgroup
-// Attention workgroups per CU over an MXFP4 pool (fp4_attn.hip): two waves per SIMD, by registers.
-constexpr int kFp4WgsPerCu = 2;
+// Attention workgroups per CU over an MXFP4 pool (fp4_attn.hip), by registers.
+__host__ __device__ constexpr int fp4_wgs_per_cu(bool few_rows) { return few_rows ? 3 : 2; }
 
 // Work-item descriptor (int32 words, one per item, fixed stride), written by the scheduler and
 // copied whole into LDS by the attention kernel:
@@ -115,6 +115,7 @@ struct AttnArgs {
   int32_t streams;         // work streams: divides Hkv and kMaxStreams
   float scale_log2;        // softmax scale * log2(e)
   bool fp4;                // pool holds MXFP4 pages (mxfp4.hpp); q and out are bf16
+  bool few_rows;           // MXFP4: most pages are read by one row tile (fp4_attn.hip)
   // Multi-query launches whose rows all have one partial: the attention kernel writes them itself,
   // as bf16 (nullptr: partial rows, folded by the merge).
   // (MXFP4 pools: decode launches as well.)

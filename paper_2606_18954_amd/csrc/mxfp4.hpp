@@ -55,7 +55,7 @@ __device__ __forceinline__ unsigned fp4_pair(unsigned w, float s) {
 // Scale byte J of w, as the float32 whose exponent it is.
 template <int J>
 __device__ __forceinline__ float fp4_exp(unsigned w) {
-  return __builtin_bit_cast(float, (J < 3 ? w << (23 - 8 * J) : w >> 1) & 0x7f800000u);
+  return __builtin_bit_cast(float, ((w >> (8 * J)) & 0xffu) << 23);
 }
 
 // Byte at bit `shift` of w, as the float32 whose exponent it is.  (A wave reads scales as whole words: a
