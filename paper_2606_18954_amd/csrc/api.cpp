@@ -355,11 +355,18 @@ void size_schedule(const ga_segment_table* st, const ga_branch_paths* bp, const 
   // workgroup) 38.6 | 42.2, 32 queries 121 | 54; merged DAGs of 24 prompts, 2 queries (56 rows, 200
   // pages a workgroup) 249 | 245; 12/12 heads x 64, 8 queries (32 rows) 269.6 | 273.6.  One query per
   // branch stays on the other kernel, whose bits decode has.
+  // MXFP4 pools cross elsewhere: a page is a quarter of the bytes, and mq_attn converts it once for its
+  // block's rows (fp4_attn.hip | mq_attn): under 64 pages a workgroup 16 step trees, 2 queries (35 rows)
+  // 49 | 51, 4 queries (70 rows) 56 | 54; one tree of 40/8 heads, 4 queries (50 rows) 30 | 18; from 64 on
+  // merged DAGs of 24 prompts, 4 queries (112 rows) 221 | 241, 8 queries (224 rows) 366 | 324; 12/12
+  // heads x 64, 16 queries (64 rows) 313 | 446.
   const bool fp4 = p->dtype == GA_MXFP4;
+  const bool full = block_pages * p->num_kv_heads >= 64 * wgs;
   const bool many_rows =
-      multi_query && (p->dtype == GA_BF16 || fp4) &&
-      (row_pages >= 128 * ref_pages ||
-       (row_pages >= 48 * ref_pages && block_pages * p->num_kv_heads >= 64 * wgs));
+      multi_query &&
+      (fp4 ? row_pages >= (full ? 144 : 48) * ref_pages
+           : p->dtype == GA_BF16 && (row_pages >= 128 * ref_pages ||
+                                     (row_pages >= 48 * ref_pages && full)));
   const int64_t work = (many_rows ? block_pages : ref_pages) * p->num_kv_heads;
   int64_t cap = (work + target_items - 1) / target_items;
   const int32_t max_cap = ga::max_chunk_pages(p->num_q_heads / p->num_kv_heads);

@@ -15,7 +15,7 @@ constexpr int kRowsPerBlock = 128;
 // Upper bound on pages per work item (the chunk's page ids are staged in LDS).
 constexpr int kMaxChunkPages = 128;
 constexpr int kAttnThreads = 256;        // 4 wave64 per workgroup
-// Attention workgroups per CU over an MXFP4 pool (fp4_attn.hip), by registers.
+// Attention workgroups per CU over an MXFP4 pool, by registers (fp4_attn.hip; mq_attn.hip has many rows).
 __host__ __device__ constexpr int fp4_wgs_per_cu(bool few_rows) { return few_rows ? 3 : 2; }
 
 // Work-item descriptor (int32 words, one per item, fixed stride), written by the scheduler and
@@ -242,7 +242,7 @@ hipError_t launch_schedule(const DevGraph& g, const DevSchedule& sc, int32_t gro
                            int32_t chunk_pages, int64_t max_items, bool reuse,
                            hipStream_t stream);
 // few_pages: a decode step with under 64 pages (times kv-heads) per workgroup at two per CU, or a
-// multi-query step with few query rows per page (bf16 steps with many run mq_attn.hip).
+// multi-query step with few query rows per page (bf16 and MXFP4 steps with many run mq_attn.hip).
 // t0 / t1 (optional, timing events): bound to the kernel's own dispatch (hipExtLaunchKernel), so
 // that their elapsed time is the kernel's execution, without the queue's gaps around it.
 hipError_t launch_seg_attn(const AttnArgs& a, int head_dim, bool bf16, bool causal,

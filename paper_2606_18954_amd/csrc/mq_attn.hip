@@ -1,4 +1,4 @@
-// Multi-query (extend, prefill) segment attention for bf16 inputs: one work item = (segment chain,
+// Multi-query (extend, prefill) segment attention for bf16 queries, bf16 or MXFP4 pools: one work item = (segment chain,
 // page chunk, row block of up to 128 query rows, kv-head), as in seg_attn.hip, with the work list,
 // the descriptors, the partial rows and the merge shared with it.
 //
@@ -36,6 +36,8 @@
 // this unit's rows are stored, and the rows leave through LDS, as whole lines.
 #include "attn_dev.hpp"
 #include "ga_internal.hpp"
+#include "mxfp4.hpp"
+#include "pool_load.hpp"
 
 #include <hip/hip_ext.h>
 
@@ -69,9 +71,18 @@ __device__ __forceinline__ int fswz(int tok) {
   return D == 128 ? ((tok & 3) << 2) | ((tok >> 2) & 3) : (((tok >> 1) & 1) << 2) | ((tok >> 2) & 3);
 }
 
-template <int D>
-__global__ __launch_bounds__(kAttnThreads, mq_wgs_per_cu(D)) void k_mq_attn(AttnArgs a) {
+// FP4: pages of an MXFP4 pool (mxfp4.hpp).  A wave's part of a slot then comes through registers, codes and
+// scales loaded an iteration before they are written to the slot as bf16, so that a page is converted once
+// for all 128 rows; what reads the slots is the same.  Two iterations ahead were slower: 20 bytes of
+// scratch at head_dim 128 (256 registers), 1448 us for the extend below where one ahead takes 1410.
+//   16-token extend as above, 1024 branches of 28/4 heads x 128: 1.41 ms (0.66 PFLOP/s) where fp4_attn.hip,
+//   whose waves convert every page for their own rows, takes 1.82 and bf16 pools 1.58 on that card.
+//   Prefill as above: 0.70 ms (0.84 PFLOP/s), fp4_attn.hip 0.87, bf16 pools 0.68.
+template <int D, bool FP4>
+__global__ __launch_bounds__(kAttnThreads, FP4 ? fp4_wgs_per_cu(false) : mq_wgs_per_cu(D)) void k_mq_attn(AttnArgs a) {
   using C = MCfg<D>;
+  using F = Fp4<D>;
+  constexpr int HEAD = FP4 ? F::PAGE : 2 * C::KVB;  // bytes of a page of one kv-head
   __shared__ __align__(1024) unsigned char smem[2 * C::SLOTS * C::HALF];   // K ring, V ring
   __shared__ __align__(1024) int s_desc[2][kDescMaxBytes / 4];
   __shared__ int s_next[2];
@@ -144,7 +155,7 @@ __global__ __launch_bounds__(kAttnThreads, mq_wgs_per_cu(D)) void k_mq_attn(Attn
   }
   __syncthreads();
 
-  const int64_t blk_stride = (int64_t)a.Hkv * 2 * C::KVB;
+  const int64_t blk_stride = (int64_t)a.Hkv * HEAD;
   const unsigned dst_w = __builtin_amdgcn_readfirstlane(lds_ring + wave * C::CPW * 1024);
   const float rgroup = 1.f / (float)a.group;
   auto page_base = [&](const unsigned char* pool_h, int word) {
@@ -166,6 +177,67 @@ __global__ __launch_bounds__(kAttnThreads, mq_wgs_per_cu(D)) void k_mq_attn(Attn
                    __builtin_amdgcn_readfirstlane(dst + i * 1024));
   };
 
+  // MXFP4: this lane's share of the wave's eight tokens (w0 ..): D / 16 bytes of K codes (token w0 + lane / 8,
+  // D / 8 channels) and of V codes (slice (lane mod 32) / 2 of two tokens from w0 + 4 (lane / 32) + 2 (lane mod
+  // 2) on), each with a word of scales.
+  struct Raw {
+    u32x2 c;
+    unsigned s;
+  };
+  const int w0 = 8 * (wave & 1);
+  const unsigned kf_off = w0 * (D / 2) + lane * (D / 16);
+  const unsigned kf_byte = (w0 + lane / 8) * F::NS + (lane % 8) * (D / 8) / 32;
+  const unsigned vf_off = F::V + (w0 / 4) * 2 * D + lane * (D / 16);
+  const unsigned vf_scale = F::VS + ((w0 / 4 + lane / 32) * F::NS + (lane % 32) / 2 * F::SL / 32) * 4;
+  auto load_raw = [&](Raw& x, const unsigned char* base, unsigned off, unsigned scale) {
+    const page_t page = page_at(base, F::PAGE);
+    if constexpr (D == 128) x.c = load8(page, off);
+    else x.c[0] = load4(page, off);
+    x.s = load4(page, scale);
+  };
+  auto load_kf = [&](Raw& x, const unsigned char* base) {
+    load_raw(x, base, kf_off, F::KS + (kf_byte & ~3u));
+  };
+  auto load_vf = [&](Raw& x, const unsigned char* base) { load_raw(x, base, vf_off, vf_scale); };
+  auto slot_row = [&](int slot, int tok) {
+    return (lds_uchar*)smem + slot * C::HALF + c_pg * C::KVB + tok * C::ROW;
+  };
+  typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+  typedef __attribute__((address_space(3))) u32x2 lds_u32x2;
+  auto put_kf = [&](const Raw& x, int slot) {
+    const float s = fp4_exp_at(x.s, 8 * (kf_byte & 3));
+    const int tok = w0 + lane / 8;
+    lds_uchar* row = slot_row(slot, tok);
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) {
+      const unsigned w = x.c[i];
+      *(lds_u32x4*)(row + (((lane % 8 * (D / 64) + i) ^ fswz<D>(tok)) << 4)) =
+          u32x4{fp4_pair<0>(w, s), fp4_pair<1>(w, s), fp4_pair<2>(w, s), fp4_pair<3>(w, s)};
+    }
+  };
+  // (a token past the page's valid ones may hold anything: its scale becomes the smallest, so that the
+  // probability 0 meets a finite value)
+  auto put_vf = [&](const Raw& x, int slot, int vm1) {
+    const int t0 = w0 + 4 * (lane / 32) + 2 * (lane % 2), r = (lane % 32) / 2;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int tok = t0 + i;
+      const unsigned sw = tok <= vm1 ? x.s : 0;
+      const float s = fp4_exp_at(sw, 16 * (lane % 2) + 8 * i);
+      lds_uchar* row = slot_row(C::SLOTS + slot, tok);
+      if constexpr (D == 128) {
+        const unsigned w = x.c[i];
+        *(lds_u32x4*)(row + ((r ^ fswz<D>(tok)) << 4)) =
+            u32x4{fp4_pair<0>(w, s), fp4_pair<1>(w, s), fp4_pair<2>(w, s), fp4_pair<3>(w, s)};
+      } else {
+        const unsigned w = x.c[0];
+        *(lds_u32x2*)(row + (((r >> 1) ^ fswz<D>(tok)) << 4) + 8 * (r & 1)) =
+            i == 0 ? u32x2{fp4_pair<0>(w, s), fp4_pair<1>(w, s)}
+                   : u32x2{fp4_pair<2>(w, s), fp4_pair<3>(w, s)};
+      }
+    }
+  };
+
   // A unit, read from its descriptor in LDS.
   struct Unit {
     int w, npe, n2, cw, row0, R, prow_base, kvh, j0;
@@ -178,6 +250,9 @@ __global__ __launch_bounds__(kAttnThreads, mq_wgs_per_cu(D)) void k_mq_attn(Attn
   const unsigned char* vq[4];                     // V bases and valid tokens of the pairs whose K
   int vqm[4];                                      // was copied, by ring slot
   int pk = 0;                                      // lane t: word of the wave's page of pair t
+  Raw rk[3], rv;                                   // MXFP4: K of pairs 0 .. 2 and V of pair 0, then
+                                                   // rk[0], rv: those an iteration ahead
+  int rvm = 0;                                     // (valid tokens of rv's page)
   auto start_unit = [&](int b) {
     Unit u;
     u.w = __builtin_amdgcn_readfirstlane(s_next[b]);
@@ -197,9 +272,21 @@ __global__ __launch_bounds__(kAttnThreads, mq_wgs_per_cu(D)) void k_mq_attn(Attn
       u.npe = max(0, min(np, (u.cw + (u.row0 + u.R - 1) / a.group + kPageTokens) / kPageTokens));
     u.n2 = (u.npe + 1) >> 1;
     u.pool_h = (const unsigned char*)uniform64(
-        (int64_t)(uintptr_t)(pool + (int64_t)u.kvh * 2 * C::KVB));
+        (int64_t)(uintptr_t)(pool + (int64_t)u.kvh * HEAD));
     // (the second page of a last pair may not exist: its first page once more, masked)
     pk = dsc[kDescHead + max(0, min(2 * lane + c_pg, u.npe - 1))];
+    if constexpr (FP4) {
+#pragma unroll
+      for (int t = 0; t < 3; ++t) {
+        const int word = __builtin_amdgcn_readlane(pk, t);
+        load_kf(rk[t], page_base(u.pool_h, word));
+        if (t == 0) {
+          load_vf(rv, page_base(u.pool_h, word));
+          rvm = (int)((unsigned)word >> kPageValidShift);
+        }
+      }
+      return u;
+    }
 #pragma unroll
     for (int t = 0; t < 5; ++t) {
       const int word = __builtin_amdgcn_readlane(pk, t);
@@ -217,6 +304,17 @@ __global__ __launch_bounds__(kAttnThreads, mq_wgs_per_cu(D)) void k_mq_attn(Attn
     return u;
   };
   auto start_rest = [&](const Unit& u) {
+    if constexpr (FP4) {
+      // The first slots' pages are written; K of pair 3 and V of pair 1 follow an iteration ahead.
+#pragma unroll
+      for (int t = 0; t < 3; ++t) put_kf(rk[t], t);
+      put_vf(rv, 0, rvm);
+      const int w3 = __builtin_amdgcn_readlane(pk, 3), w1 = __builtin_amdgcn_readlane(pk, 1);
+      load_kf(rk[0], page_base(u.pool_h, w3));
+      load_vf(rv, page_base(u.pool_h, w1));
+      rvm = (int)((unsigned)w1 >> kPageValidShift);
+      return;
+    }
     if (3 < u.n2) copy_k(vq[3] - C::KVB, dst_w + 3 * C::HALF);
     if (2 < u.n2) copy_v(vq[2], vqm[2], dst_w + (C::SLOTS + 2) * C::HALF);
   };
@@ -268,10 +366,13 @@ __global__ __launch_bounds__(kAttnThreads, mq_wgs_per_cu(D)) void k_mq_attn(Attn
 
     // The first copies, the queries and the claim have landed; the row stores of the unit before,
     // issued after them, need not have.
-    if (stored) wait_vmcnt_const<kStores>();
-    else wait_vmcnt(0);
+    if (!FP4) {
+      if (stored) wait_vmcnt_const<kStores>();
+      else wait_vmcnt(0);
+    }
     asm volatile("" : "+v"(claim));
-    wg_barrier();                       // every wave's first copies have landed, and its rows of
+    if (FP4) lds_barrier();
+    else wg_barrier();                  // every wave's first copies have landed, and its rows of
                                         // the unit before no longer need that unit's descriptor
     if (wave == 0) {
       int v;
@@ -407,6 +508,23 @@ __global__ __launch_bounds__(kAttnThreads, mq_wgs_per_cu(D)) void k_mq_attn(Attn
     // ring slots are compile-time, U = it mod 4).
     auto iteration = [&](auto live, auto ut, int it) {
       constexpr int U = decltype(ut)::value;
+      if constexpr (FP4) {
+        constexpr int K3 = (U + 3) & 3, V1 = (U + 1) & 3;
+        lds_barrier();                               // (every wave is done with both slots)
+        if (it + 3 < n2) put_kf(rk[0], K3);
+        if (it + 1 < n2) put_vf(rv, V1, rvm);
+        const int wk = __builtin_amdgcn_readlane(pk, min(it + 4, 63));
+        const int wv = __builtin_amdgcn_readlane(pk, min(it + 2, 63));
+        load_kf(rk[0], page_base(u.pool_h, wk));     // (past the end: the last page once more)
+        load_vf(rv, page_base(u.pool_h, wv));
+        rvm = (int)((unsigned)wv >> kPageValidShift);
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (decltype(live)::value) {
+          if ((masked >> it) & 1) mask(it);
+          body(ut, std::integral_constant<int, (U + 2) & 3>{}, it);
+        }
+        return;
+      }
       if (it + 5 <= n2) {
         wait_vmcnt_const<4 * C::CPW>();
       } else {
@@ -442,7 +560,7 @@ __global__ __launch_bounds__(kAttnThreads, mq_wgs_per_cu(D)) void k_mq_attn(Attn
         for (int s = 0; s < C::KS; ++s) read_k(std::integral_constant<int, 1>{}, s);
       }
       lds_barrier();                               // the first two K slots are free
-      if (n2 > 4) copy_k(vq[0] - C::KVB, dst_w);
+      if (!FP4 && n2 > 4) copy_k(vq[0] - C::KVB, dst_w);
       for (int it = 0; it < n2; it += 4) {
         iteration(live, std::integral_constant<int, 0>{}, it);
         if (it + 1 >= n2) break;
@@ -576,12 +694,12 @@ __global__ __launch_bounds__(kAttnThreads, mq_wgs_per_cu(D)) void k_mq_attn(Attn
   }
 }
 
-template <int D>
+template <int D, bool FP4>
 hipError_t launch_t(const AttnArgs& a, int grid, hipStream_t stream, hipEvent_t t0, hipEvent_t t1) {
   if (t0 || t1)
-    hipExtLaunchKernelGGL(k_mq_attn<D>, dim3(grid), dim3(kAttnThreads), 0, stream, t0, t1, 0, a);
+    hipExtLaunchKernelGGL((k_mq_attn<D, FP4>), dim3(grid), dim3(kAttnThreads), 0, stream, t0, t1, 0, a);
   else
-    hipLaunchKernelGGL(k_mq_attn<D>, dim3(grid), dim3(kAttnThreads), 0, stream, a);
+    hipLaunchKernelGGL((k_mq_attn<D, FP4>), dim3(grid), dim3(kAttnThreads), 0, stream, a);
   return hipGetLastError();
 }
 
@@ -589,8 +707,13 @@ hipError_t launch_t(const AttnArgs& a, int grid, hipStream_t stream, hipEvent_t 
 
 hipError_t launch_mq_attn(const AttnArgs& a, int head_dim, int grid, hipStream_t stream,
                           hipEvent_t t0, hipEvent_t t1) {
-  if (head_dim == 64) return launch_t<64>(a, grid, stream, t0, t1);
-  if (head_dim == 128) return launch_t<128>(a, grid, stream, t0, t1);
+  if (a.fp4) {
+    if (head_dim == 64) return launch_t<64, true>(a, grid, stream, t0, t1);
+    if (head_dim == 128) return launch_t<128, true>(a, grid, stream, t0, t1);
+    return hipErrorInvalidValue;
+  }
+  if (head_dim == 64) return launch_t<64, false>(a, grid, stream, t0, t1);
+  if (head_dim == 128) return launch_t<128, false>(a, grid, stream, t0, t1);
   return hipErrorInvalidValue;
 }
 

@@ -737,7 +737,7 @@ int seg_attn_grid(int head_dim, bool bf16, bool causal, bool few_pages, int num_
 hipError_t launch_seg_attn(const AttnArgs& a, int head_dim, bool bf16, bool causal,
                            bool few_pages, int grid, hipStream_t stream, hipEvent_t t0,
                            hipEvent_t t1) {
-  if (a.fp4) return launch_fp4_attn(a, head_dim, causal, grid, stream, t0, t1);
+  if (a.fp4 && (few_pages || !causal)) return launch_fp4_attn(a, head_dim, causal, grid, stream, t0, t1);
   if (bf16 && causal && !few_pages) return launch_mq_attn(a, head_dim, grid, stream, t0, t1);
   if (bf16) {
     if (head_dim == 64) return launch_t<64, true>(a, causal, few_pages, grid, stream, t0, t1);

@@ -277,6 +277,37 @@ def test_prefill_of_many_rows():
     check_attention("prefill of many rows", out, lse, q, vals, g, 28, 4, lens, sorted(rows))
 
 
+@pytest.mark.parametrize("Hq,Hkv,D", HEADS)
+@pytest.mark.parametrize("prefix,step", [(1, 33), (259, 40), (900, 17)])
+def test_many_query_rows_a_page(Hq, Hkv, D, prefix, step):
+    """Branches of up to `step` queries over a shared prefix: row blocks of 128 rows and less, pages that end
+    inside a tile with NaN scales behind, one partial row (prefix 1) and several."""
+    require_gpu()
+    rng = np.random.default_rng(Hq * prefix + step)
+    own = [int(n) for n in rng.integers(1, step + 1, 9)]
+    own[0], own[1] = step, 1
+    lens, paths = W.with_new_steps([prefix, 18], [[0]] * 8 + [[0, 1]], own)
+    g = W.assemble_graph(lens, paths, 6, slack_pages=2)
+    say(f"[case] extend {Hq}/{Hkv}/{D} prefix {prefix} counts {own}")
+    raw, vals, q = _case(rng, g, Hq, Hkv, D, sum(own))
+    out, lse = _run(g, raw, q, Hq, Hkv, D, own)
+    check_attention(f"many rows {Hq}/{Hkv}/{D}", out, lse, q, vals, g, Hq, Hkv, own)
+
+
+@pytest.mark.parametrize("Hq,Hkv,D", HEADS)
+def test_few_query_rows_a_page(Hq, Hkv, D):
+    """One to three queries a branch, mostly over pages of their own."""
+    require_gpu()
+    rng = np.random.default_rng(Hq)
+    own = [1, 2, 3, 2, 1]
+    lens, paths = W.with_new_steps([5, 300, 130, 77, 16, 201], [[0, 1], [0, 2], [3], [4], [5]], own)
+    g = W.assemble_graph(lens, paths, 6, slack_pages=2)
+    say(f"[case] extend {Hq}/{Hkv}/{D} counts {own}")
+    raw, vals, q = _case(rng, g, Hq, Hkv, D, sum(own))
+    out, lse = _run(g, raw, q, Hq, Hkv, D, own)
+    check_attention(f"few rows {Hq}/{Hkv}/{D}", out, lse, q, vals, g, Hq, Hkv, own)
+
+
 def test_entry_points_agree_bit_for_bit():
     """decode, decode_static, a plan, a plan with one query each and a later run of it: the same bits."""
     require_gpu()
