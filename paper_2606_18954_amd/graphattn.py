@@ -191,11 +191,26 @@ def make_params(num_q_heads: int, num_kv_heads: int, head_dim: int, num_pages: i
                   DTYPES.get(dtype, GA_F32), softmax_scale, int(bool(out_f32)))
 
 
-def _stream_handle(stream) -> int:
+def _stream_getter():
+    """The function that gives the current stream's handle.  torch's raw getter, where it has one: a Stream
+    object costs 2.7 us, a third of a call that launches one small kernel; the getter 0.2 us."""
     import torch
-    if stream is None:
-        stream = torch.cuda.current_stream()
-    return int(stream.cuda_stream)
+    device, raw = torch.cuda.current_device, getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    if raw is None:
+        return lambda: int(torch.cuda.current_stream().cuda_stream)
+    return lambda: int(raw(device()))
+
+
+_current_stream = None
+
+
+def _stream_handle(stream) -> int:
+    global _current_stream
+    if stream is not None:
+        return int(stream.cuda_stream)
+    if _current_stream is None:
+        _current_stream = _stream_getter()
+    return _current_stream()
 
 
 def _dev_ptr(t) -> int:
