@@ -3,14 +3,19 @@
 //
 // Keys order like the masses: the float's bits, negative ones inverted and positive ones with the sign
 // bit set; -0 counts as 0, a NaN above every number (its weight is unknown: the token stays), and a
-// protected token above that.  The keep-th largest key T is built bit by bit from the top (the largest
-// T that at least keep keys reach); a step is one comparison and one ballot for 64 keys, and the
-// search ends early once exactly keep keys reach the candidate.  Then every key above T stays and, in
-// order of position, as many of those equal to T as are missing.
+// protected token above that.  With need = keep - (protected tokens), the search keeps a lower key that at
+// least need of the other keys reach and an upper one that fewer reach, and counts how many reach a key
+// between them, where the line through the two counts meets need.  A step is one comparison and one ballot
+// for 64 keys.  Where at most 64 keys are left between the bounds they are gathered in LDS, one a lane, and
+// ranked against each other.  Zeros (tokens that no row saw) lie far below all other masses: the search
+// begins above them where enough keys do.  Masses of a softmax take three steps at 500 tokens and six at
+// 8,000 (bit by bit it took 14 and 18); every other step after the twelfth halves the range, so that 76 end
+// it whatever the masses are.  Then every key above T stays and, in order of position, as many of those
+// equal to T as are missing.
 //
 // Segments of up to kEvictWave tokens: one wave each, keys and words in registers, no barrier.  Up to
-// kEvictGroup: one workgroup of 1024 threads, a barrier a bit.  Longer ones: the same, but the keys are
-// read again for every bit.
+// kEvictGroup: one workgroup of 1024 threads, a barrier a step.  Longer ones: the same, but the keys are
+// read again for every step.
 #include "evict_internal.hpp"
 
 namespace ga {
@@ -22,14 +27,24 @@ __device__ __forceinline__ unsigned key_of(float x) {
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-// Word and key of token t (key 0, below every token's, past the segment's end).
-__device__ __forceinline__ void token(const EvictArgs& a, const EvictSeg& s, int t, int& word,
-                                      unsigned& key) {
-  word = 0;
-  key = 0;
-  if (t < s.len) {
-    word = a.pages[s.pages + (t >> 4)] * kPageTokens + (t & 15);
-    key = t < a.first || t >= s.len - a.recent ? 0xffffffffu : key_of(a.mass[word]);
+// Words and keys of N tokens from t on, STEP apart (key 0, below every token's, past the segment's end: those
+// lanes load the last token's, so that every load is issued before the first is waited for).
+template <int N, int STEP>
+__device__ __forceinline__ void tokens(const EvictArgs& a, const EvictSeg& s, int t, int* word,
+                                       unsigned* key) {
+  float m[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int u = min(t + STEP * i, s.len - 1);
+    word[i] = a.pages[s.pages + (u >> 4)] * kPageTokens + (u & 15);
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) m[i] = a.mass[word[i]];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int u = t + STEP * i;
+    key[i] = u < a.first || u >= s.len - a.recent ? 0xffffffffu : key_of(m[i]);
+    if (u >= s.len) key[i] = 0;
   }
 }
 
@@ -37,104 +52,263 @@ __device__ __forceinline__ int below(uint64_t m, int lane) {
   return __builtin_popcountll(m & ((1ull << lane) - 1));
 }
 
+constexpr unsigned kZeroKey = 0x80000000u;           // of no mass, and of -0
+
+// The search's bounds: of the unprotected keys clo >= need reach lo, chi < need reach hi.  A bound that stays
+// twice weighs half as much in the next line (an uneven spread of the keys would keep one for many steps).
+struct Bounds {
+  unsigned lo, hi;
+  int clo, chi;
+  float wlo = 1.f, whi = 1.f;
+  int last = 0;
+  __device__ __forceinline__ bool closed(int need) const { return clo == need || hi - lo == 1; }
+  __device__ __forceinline__ bool far(int need) const { return !closed(need) && clo - chi > 64; }
+  __device__ __forceinline__ bool holds(unsigned k) const { return k - lo < hi - lo; }
+  // The step's key, in (lo, hi).
+  __device__ __forceinline__ unsigned next(int need, int step) const {
+    const unsigned span = hi - lo;
+    if (step == 0 && hi == kZeroKey + 1) return kZeroKey;   // (often they are all zero)
+    if (step >= 12 && (step & 1)) return lo + span / 2;
+    const float b = ((float)(clo - need) + 0.5f) * wlo, t = ((float)(need - chi) - 0.5f) * whi;
+    const float at = (float)span * (b * __builtin_amdgcn_rcpf(b + t));
+    // (a product that rounds up to the span is kept below it)
+    return lo + min(max((unsigned)fminf(at, 4.2e9f), 1u), span - 1);
+  }
+  __device__ __forceinline__ void set(unsigned x, int c, int need) {
+    if (c >= need) {
+      lo = x;
+      clo = c;
+      wlo = 1.f;
+      whi = last > 0 ? 0.5f * whi : 1.f;
+      last = 1;
+    } else {
+      hi = x;
+      chi = c;
+      whi = 1.f;
+      wlo = last < 0 ? 0.5f * wlo : 1.f;
+      last = -1;
+    }
+  }
+};
+
+// Among the m = clo - chi <= 64 keys between the bounds, one a lane (0: none), the one at which need is reached
+// becomes the lower bound, with its neighbour above.
+__device__ __forceinline__ void rank_rest(Bounds& x, unsigned mine, int need) {
+  const int m = x.clo - x.chi, want = need - x.chi;
+  int above = 0, reach = 0;
+  for (int j = 0; j < m; ++j) {
+    const unsigned k = __builtin_amdgcn_readlane(mine, j);
+    above += k > mine;
+    reach += k >= mine;
+  }
+  const uint64_t at = __ballot(mine != 0 && above < want && want <= reach);
+  const int l = __builtin_ctzll(at);
+  x.lo = __builtin_amdgcn_readlane(mine, l);
+  x.hi = x.lo + 1;
+  x.clo = x.chi + __builtin_amdgcn_readlane(reach, l);
+  x.chi += __builtin_amdgcn_readlane(above, l);
+}
+
+// The bounds the search begins with: of n open keys pos lie above zero's, kmin .. kmax.  (Below them no key is
+// under 0x7fffff, minus infinity's.)
+__device__ __forceinline__ Bounds first_bounds(int n, int pos, unsigned kmin, unsigned kmax, int need) {
+  if (pos >= need) return Bounds{kmin, kmax + 1, pos, 0};
+  return Bounds{1, kZeroKey + 1, n, pos};
+}
+
+__device__ __forceinline__ bool positive_key(unsigned k) { return k > kZeroKey && k != 0xffffffffu; }
+
+__device__ __forceinline__ void wave_min_max(unsigned& lo, unsigned& hi) {
+#pragma unroll
+  for (int d = 32; d; d /= 2) {
+    lo = min(lo, (unsigned)__shfl_xor((int)lo, d));
+    hi = max(hi, (unsigned)__shfl_xor((int)hi, d));
+  }
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  hi = __builtin_amdgcn_readfirstlane(hi);
+}
+
+// LDS written by a wave's lanes, read by its others.
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 __global__ __launch_bounds__(256) void k_evict_wave(EvictArgs a) {
-  constexpr int NK = kEvictWave / 64;
-  const int lane = threadIdx.x & 63;
-  const int id = (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  constexpr int NK = kEvictWave / 64, NB = 4;        // keys a lane, in runs of NB that a segment has or not
+  __shared__ unsigned s_rest[4][64];                 // (each wave has its own: no barrier)
+  __shared__ int s_num[4];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int id = (int)blockIdx.x * 4 + wave;
   if (id >= a.n_wave) return;
+  s_rest[wave][lane] = 0;
+  if (lane == 0) s_num[wave] = 0;
+  wave_sync();
   const EvictSeg s = a.segs[id];
   int word[NK];
   unsigned key[NK];
+  unsigned kmin = 0xffffffffu, kmax = 0;
+  int pos = 0;
+  auto runs = [&](auto f) {
 #pragma unroll
-  for (int i = 0; i < NK; ++i) token(a, s, 64 * i + lane, word[i], key[i]);
-  unsigned T = 0;
-  int reach = 0;
-  if (s.keep > 0)
-    for (int bit = 31; bit >= 0; --bit) {
-      const unsigned cand = T | (1u << bit);
-      int c = 0;
+    for (int b = 0; b < NK; b += NB)
+      if (64 * b < s.len) f(b);
+  };
+  runs([&](int b) {
+    tokens<NB, 64>(a, s, 64 * b + lane, word + b, key + b);
+  });
+  runs([&](int b) {
 #pragma unroll
-      for (int i = 0; i < NK; ++i) c += __builtin_popcountll(__ballot(key[i] >= cand));
-      if (c >= s.keep) {
-        T = cand;
-        reach = c;
-        if (c == s.keep) break;
-      }
+    for (int i = b; i < b + NB; ++i) {
+      const bool p = positive_key(key[i]);
+      pos += __builtin_popcountll(__ballot(p));
+      kmin = min(kmin, p ? key[i] : 0xffffffffu);
+      kmax = max(kmax, p ? key[i] : 0);
     }
-  else
-    T = 0xffffffffu;
-  // Keys that reach T all stay where they are as many as wanted; else those equal to it only as far
-  // as wanted.
-  int above = 0;
-  if (s.keep > 0 && reach != s.keep) {
+  });
+  const int safe = (int)min((int64_t)s.len, (int64_t)a.first + a.recent);
+  const int need = s.keep - safe;
+  unsigned T = 0xfffffffeu;                          // keys above T stay, and `ties` of those equal to it
+  int ties = 0;
+  if (need > 0) {
+    wave_min_max(kmin, kmax);
+    Bounds x = first_bounds(s.len - safe, pos, kmin, kmax, need);
+    for (int step = 0; x.far(need); ++step) {
+      const unsigned k = __builtin_amdgcn_readfirstlane(x.next(need, step));
+      int c = -safe;                                 // (protected keys reach every k)
+      runs([&](int b) {
 #pragma unroll
-    for (int i = 0; i < NK; ++i) above += __builtin_popcountll(__ballot(key[i] > T));
+        for (int i = b; i < b + NB; ++i) c += __builtin_popcountll(__ballot(key[i] >= k));
+      });
+      x.set(k, c, need);
+    }
+    if (!x.closed(need)) {
+      runs([&](int b) {
+#pragma unroll
+        for (int i = b; i < b + NB; ++i)
+          if (x.holds(key[i])) s_rest[wave][atomicAdd(&s_num[wave], 1)] = key[i];
+      });
+      wave_sync();
+      rank_rest(x, s_rest[wave][lane], need);
+    }
+    T = x.clo == need ? x.lo - 1 : x.lo;
+    ties = x.clo == need ? 0 : need - x.chi;
   }
-  int ties = s.keep > 0 ? (reach == s.keep ? 0x7fffffff : s.keep - above) : 0;
   int64_t out = s.out;
+  runs([&](int b) {
 #pragma unroll
-  for (int i = 0; i < NK; ++i) {
-    const bool eq = key[i] == T && key[i] != 0;
-    const uint64_t me = __ballot(eq);
-    const bool stay = key[i] > T || (eq && below(me, lane) < ties);
-    ties -= min(ties, (int)__builtin_popcountll(me));
-    const uint64_t ms = __ballot(stay);
-    if (stay) {
-      const int64_t o = out + below(ms, lane);
-      if (a.positions) a.positions[o] = 64 * i + lane;
-      if (a.words) a.words[o] = word[i];
+    for (int i = b; i < b + NB; ++i) {
+      const bool eq = ties > 0 && key[i] == T;
+      const uint64_t me = __ballot(eq);
+      const bool stay = key[i] > T || (eq && below(me, lane) < ties);
+      ties -= min(ties, (int)__builtin_popcountll(me));
+      const uint64_t ms = __ballot(stay);
+      if (stay) {
+        const int64_t o = out + below(ms, lane);
+        if (a.positions) a.positions[o] = 64 * i + lane;
+        if (a.words) a.words[o] = word[i];
+      }
+      out += __builtin_popcountll(ms);
     }
-    out += __builtin_popcountll(ms);
-  }
+  });
 }
 
 // One workgroup of 16 waves per segment.
 template <bool LONG>
 __global__ __launch_bounds__(1024) void k_evict_group(EvictArgs a) {
-  constexpr int NK = 16;
-  __shared__ int s_cnt[33];
+  constexpr int NK = 16, NB = 4;
+  __shared__ int s_cnt[3];                           // counts of three steps in turn
+  __shared__ int s_sum[2], s_pos, s_num;
+  __shared__ unsigned s_rest[64];
+  __shared__ unsigned s_min, s_max;
   __shared__ int s_gt[NK * 16], s_eq[NK * 16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const EvictSeg s = a.segs[a.n_wave + (LONG ? a.n_group : 0) + (int)blockIdx.x];
   const int nblk = LONG ? (s.len + kEvictGroup - 1) / kEvictGroup : 1;
-  if (tid < 33) s_cnt[tid] = 0;
-  int word[NK];
+  if (tid < 3) s_cnt[tid] = 0;
+  if (tid < 64) s_rest[tid] = 0;
+  if (tid == 0) {
+    s_pos = s_num = 0;
+    s_min = 0xffffffffu;
+    s_max = 0;
+  }
+  int word[NK] = {};
   unsigned key[NK];
+  auto runs = [&](int blk, auto f) {
+#pragma unroll
+    for (int b = 0; b < NK; b += NB)
+      if (blk * kEvictGroup + 1024 * b < s.len) f(b);
+  };
   auto load = [&](int blk) {
 #pragma unroll
-    for (int i = 0; i < NK; ++i)
-      token(a, s, blk * kEvictGroup + 1024 * i + tid, word[i], key[i]);
+    for (int i = 0; i < NK; ++i) key[i] = 0;
+    runs(blk, [&](int b) {
+      tokens<NB, 1024>(a, s, blk * kEvictGroup + 1024 * b + tid, word + b, key + b);
+    });
   };
   load(0);
-  __syncthreads();
-  unsigned T = 0;
-  int reach = 0;
-  // Keys of the whole segment that reach x, through counter slot k.
-  auto count = [&](unsigned x, int k) {
-    int c = 0;
-    for (int blk = 0; blk < nblk; ++blk) {
-      if (LONG) load(blk);
-#pragma unroll
-      for (int i = 0; i < NK; ++i) c += __builtin_popcountll(__ballot(key[i] >= x));
-    }
-    if (lane == 0) atomicAdd(&s_cnt[k], c);
-    __syncthreads();
-    return s_cnt[k];
-  };
-  if (s.keep > 0)
-    for (int bit = 31; bit >= 0; --bit) {
-      const unsigned cand = T | (1u << bit);
-      const int c = count(cand, bit);
-      if (c >= s.keep) {
-        T = cand;
-        reach = c;
-        if (c == s.keep) break;
-      }
-    }
-  else
-    T = 0xffffffffu;
+  const int safe = (int)min((int64_t)s.len, (int64_t)a.first + a.recent);
+  const int need = s.keep - safe;
+  unsigned T = 0xfffffffeu;
   int ties = 0;
-  if (s.keep > 0) ties = reach == s.keep ? 0x7fffffff : s.keep - (T == 0xffffffffu ? 0 : count(T + 1, 32));
+  __syncthreads();
+  if (need > 0) {
+    unsigned kmin = 0xffffffffu, kmax = 0;
+    int pos = 0;
+    for (int blk = 0; blk < nblk; ++blk) {
+      if (LONG && blk) load(blk);
+      runs(blk, [&](int b) {
+#pragma unroll
+        for (int i = b; i < b + NB; ++i) {
+          const bool p = positive_key(key[i]);
+          pos += __builtin_popcountll(__ballot(p));
+          kmin = min(kmin, p ? key[i] : 0xffffffffu);
+          kmax = max(kmax, p ? key[i] : 0);
+        }
+      });
+    }
+    wave_min_max(kmin, kmax);
+    if (lane == 0) {
+      atomicAdd(&s_pos, pos);
+      atomicMin(&s_min, kmin);
+      atomicMax(&s_max, kmax);
+    }
+    __syncthreads();
+    Bounds x = first_bounds(s.len - safe, __builtin_amdgcn_readfirstlane(s_pos),
+                            __builtin_amdgcn_readfirstlane(s_min),
+                            __builtin_amdgcn_readfirstlane(s_max), need);
+    for (int step = 0, k3 = 0; x.far(need); ++step, k3 = k3 == 2 ? 0 : k3 + 1) {
+      const unsigned k = __builtin_amdgcn_readfirstlane(x.next(need, step));
+      int c = 0;
+      for (int blk = 0; blk < nblk; ++blk) {
+        if (LONG) load(blk);
+        runs(blk, [&](int b) {
+#pragma unroll
+          for (int i = b; i < b + NB; ++i) c += __builtin_popcountll(__ballot(key[i] >= k));
+        });
+      }
+      if (lane == 0) atomicAdd(&s_cnt[k3], c);
+      __syncthreads();
+      // The last step's counter is cleared: its readers are past this barrier, its next writers behind the
+      // next one.
+      if (tid == 0) s_cnt[k3 == 0 ? 2 : k3 - 1] = 0;
+      x.set(k, __builtin_amdgcn_readfirstlane(s_cnt[k3]) - safe, need);
+    }
+    if (!x.closed(need)) {
+      for (int blk = 0; blk < nblk; ++blk) {
+        if (LONG) load(blk);
+        runs(blk, [&](int b) {
+#pragma unroll
+          for (int i = b; i < b + NB; ++i)
+            if (x.holds(key[i])) s_rest[atomicAdd(&s_num, 1)] = key[i];
+        });
+      }
+      __syncthreads();
+      rank_rest(x, s_rest[lane], need);
+    }
+    T = x.clo == need ? x.lo - 1 : x.lo;
+    ties = x.clo == need ? 0 : need - x.chi;
+  }
   int64_t out = s.out;
   for (int blk = 0; blk < nblk; ++blk) {
     if (LONG) load(blk);
@@ -142,7 +316,7 @@ __global__ __launch_bounds__(1024) void k_evict_group(EvictArgs a) {
 #pragma unroll
     for (int i = 0; i < NK; ++i) {
       const int g = __builtin_popcountll(__ballot(key[i] > T));
-      const int e = __builtin_popcountll(__ballot(key[i] == T && key[i] != 0));
+      const int e = __builtin_popcountll(__ballot(ties > 0 && key[i] == T));
       if (lane == 0) {
         s_gt[16 * i + wave] = g;
         s_eq[16 * i + wave] = e;
@@ -175,15 +349,15 @@ __global__ __launch_bounds__(1024) void k_evict_group(EvictArgs a) {
         pe += e[k];
       }
       if (lane == 63) {
-        s_cnt[0] = pg;            // (the bits' counters are no longer needed)
-        s_cnt[1] = pe;
+        s_sum[0] = pg;
+        s_sum[1] = pe;
       }
     }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < NK; ++i) {
       const int pg = s_gt[16 * i + wave], pe = s_eq[16 * i + wave];
-      const bool eq = key[i] == T && key[i] != 0;
+      const bool eq = ties > 0 && key[i] == T;
       const uint64_t me = __ballot(eq);
       const bool stay = key[i] > T || (eq && pe + below(me, lane) < ties);
       const uint64_t ms = __ballot(stay);
@@ -193,7 +367,7 @@ __global__ __launch_bounds__(1024) void k_evict_group(EvictArgs a) {
         if (a.words) a.words[o] = word[i];
       }
     }
-    const int tg = s_cnt[0], te = min(s_cnt[1], ties);
+    const int tg = s_sum[0], te = min(s_sum[1], ties);
     out += tg + te;
     ties -= te;
     __syncthreads();
