@@ -18,9 +18,15 @@
 // which rounding to it is as near as to the next one: no value is clipped by more than a rounding),
 // kept in [-125, 125] so that every value of the block is a normal float32; x / 2^e is rounded to the
 // nearest code, ties to the even one, by the conversion instruction.  A block with a NaN or an
-// infinity has scale byte 255 and reads as NaN.
+// infinity has scale byte 255 and reads as NaN.  Memory bounds it: 32768 tokens of 8 heads x 128 in random
+// order, 169 MB, append 44.8 us (3.8 TB/s), read 37.2 (4.5; a plain copy reaches 5.15 on that card).  The
+// bf16 rows pass the caches by (non-temporal), so that a page's lines, which four tokens' V share, stay until
+// all have come: with ordinary loads and stores the two take 96 us, not 82.  Two tokens a thread (82 us) hide
+// the latency of the words better than one (85) and leave a step's 1024 tokens more workgroups than four (a
+// step's append and read 10.4 us, 12.0 with four).
 #include "ga_internal.hpp"
 #include "mxfp4.hpp"
+#include "pool_load.hpp"
 
 namespace ga {
 namespace {
@@ -74,57 +80,84 @@ __device__ __forceinline__ void store_codes(unsigned char* blk, int t, int c, bo
   }
 }
 
-// MODE 0: append, 1: copy, 2: read.
+// MODE 0: append, 1: copy, 2: read.  A thread takes 8 channels of kPieces tokens' K or V, which D / 8 threads
+// share: each kind of load is issued for all of them before the first is used.
+constexpr int kPieces = 2;
+
 template <int D, int MODE>
 __global__ __launch_bounds__(256) void k_kv_fp4(KvWriteArgs a) {
-  const int64_t gid = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  constexpr int PR = D / 8;                          // threads of a token's K or V
-  const int ppt = a.Hkv * 2 * PR;
-  const int64_t j = gid / ppt;
-  if (j >= a.n) return;
-  const int p = (int)(gid - j * ppt);
-  const int h = p / (2 * PR), c = 8 * (p % PR);
-  const bool v = (p / PR) & 1;
-  const int32_t dw = a.dst_words[j];
-  if (dw < 0 || (int64_t)dw >= a.num_slots) return;  // (the four lanes of a block go together)
-  unsigned char* dst = a.pool + ((int64_t)(dw >> 4) * a.Hkv + h) * Fp4<D>::PAGE;
-  const int td = dw & 15;
-  const int64_t row = ((j * a.Hkv + h) * D + c) * 2; // of k_new / v_new, k_out / v_out
-  if constexpr (MODE == 0) {
-    const uint4 x = *reinterpret_cast<const uint4*>((v ? a.v_new : a.k_new) + row);
-    const unsigned w[4] = {x.x, x.y, x.z, x.w};
-    // bf16 magnitudes order like the integers they are.
-    unsigned top = 0;
+  constexpr int PR = D / 8, UB = 256 / PR;           // threads of a token's K or V, of which a block has UB
+  const int per = 2 * a.Hkv, c = 8 * ((int)threadIdx.x % PR);
+  const int64_t first = (int64_t)blockIdx.x * (kPieces * UB), j0 = first / per;
+  const unsigned r0 = (unsigned)(first - j0 * per) + threadIdx.x / PR;
+  int64_t row[kPieces];                              // of k_new / v_new, k_out / v_out
+  int h[kPieces];
+  bool v[kPieces], ok[kPieces];
+  int32_t dw[kPieces], sw[kPieces];
+  u32x4 x[kPieces];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) top = max(top, max(w[i] & 0x7fffu, (w[i] >> 16) & 0x7fffu));
-    top = max(top, (unsigned)__shfl_xor((int)top, 1));
-    top = max(top, (unsigned)__shfl_xor((int)top, 2));
-    // Exponent of a, plus one from mantissa 0.75 on; two below it is the scale.
-    int byte = (int)((top + 0x20u) >> 7) - 2;
-    byte = top >= 0x7f80u ? 255 : min(max(byte, 2), 252);
-    unsigned code = 0;
-    if (byte != 255) {
-      const float s = __builtin_bit_cast(float, (unsigned)byte << 23);
-      code = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code, __builtin_bit_cast(bf16x2_t, w[0]), s, 0);
-      code = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code, __builtin_bit_cast(bf16x2_t, w[1]), s, 1);
-      code = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code, __builtin_bit_cast(bf16x2_t, w[2]), s, 2);
-      code = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code, __builtin_bit_cast(bf16x2_t, w[3]), s, 3);
+  for (int i = 0; i < kPieces; ++i) {
+    const unsigned r = r0 + i * UB, dj = r / (unsigned)per, hv = r - dj * per;
+    const int64_t j = j0 + dj;
+    ok[i] = j < a.n;                                 // (the four lanes of a block go together)
+    h[i] = (int)(hv >> 1);
+    v[i] = hv & 1;
+    row[i] = ((j * a.Hkv + h[i]) * D + c) * 2;
+    dw[i] = ok[i] ? a.dst_words[j] : -1;
+    if constexpr (MODE == 1) sw[i] = ok[i] ? a.src_words[j] : -1;
+    if constexpr (MODE == 0)
+      if (ok[i])
+        x[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>((v[i] ? a.v_new : a.k_new) + row[i]));
+  }
+  auto block = [&](int32_t w, int i) {
+    return a.pool + ((int64_t)(w >> 4) * a.Hkv + h[i]) * Fp4<D>::PAGE;
+  };
+  unsigned code[kPieces], byte[kPieces];
+#pragma unroll
+  for (int i = 0; i < kPieces; ++i) {
+    ok[i] = dw[i] >= 0 && (int64_t)dw[i] < a.num_slots;
+    if constexpr (MODE == 1) ok[i] = ok[i] && sw[i] >= 0 && (int64_t)sw[i] < a.num_slots;
+    if constexpr (MODE != 0)
+      if (ok[i]) {
+        const int32_t w = MODE == 1 ? sw[i] : dw[i];
+        const unsigned char* src = block(w, i);
+        code[i] = load_codes<D>(src, w & 15, c, v[i]);
+        byte[i] = src[fp4_scale<D>(w & 15, c, v[i])];
+      }
+  }
+#pragma unroll
+  for (int i = 0; i < kPieces; ++i) {
+    if (!ok[i]) continue;
+    if constexpr (MODE == 0) {
+      const unsigned w[4] = {x[i][0], x[i][1], x[i][2], x[i][3]};
+      // bf16 magnitudes order like the integers they are.
+      unsigned top = 0;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) top = max(top, max(w[k] & 0x7fffu, (w[k] >> 16) & 0x7fffu));
+      top = max(top, (unsigned)__shfl_xor((int)top, 1));
+      top = max(top, (unsigned)__shfl_xor((int)top, 2));
+      // Exponent of a, plus one from mantissa 0.75 on; two below it is the scale.
+      byte[i] = (unsigned)min(max((int)((top + 0x20u) >> 7) - 2, 2), 252);
+      const float s = __builtin_bit_cast(float, byte[i] << 23);
+      unsigned q = 0;
+      q = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(q, __builtin_bit_cast(bf16x2_t, w[0]), s, 0);
+      q = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(q, __builtin_bit_cast(bf16x2_t, w[1]), s, 1);
+      q = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(q, __builtin_bit_cast(bf16x2_t, w[2]), s, 2);
+      q = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(q, __builtin_bit_cast(bf16x2_t, w[3]), s, 3);
+      const bool nan = top >= 0x7f80u;
+      code[i] = nan ? 0 : q;
+      if (nan) byte[i] = 255;
     }
-    store_codes<D>(dst, td, c, v, code);
-    if ((c & 31) == 0) dst[fp4_scale<D>(td, c, v)] = (unsigned char)byte;
-  } else if constexpr (MODE == 1) {
-    const int32_t sw = a.src_words[j];
-    if (sw < 0 || (int64_t)sw >= a.num_slots) return;
-    const unsigned char* src = a.pool + ((int64_t)(sw >> 4) * a.Hkv + h) * Fp4<D>::PAGE;
-    const int ts = sw & 15;
-    store_codes<D>(dst, td, c, v, load_codes<D>(src, ts, c, v));
-    if ((c & 31) == 0) dst[fp4_scale<D>(td, c, v)] = src[fp4_scale<D>(ts, c, v)];
-  } else {
-    const unsigned code = load_codes<D>(dst, td, c, v);
-    const float s = __builtin_bit_cast(float, (unsigned)dst[fp4_scale<D>(td, c, v)] << 23);
-    *reinterpret_cast<uint4*>((v ? a.v_out : a.k_out) + row) =
-        make_uint4(fp4_pair<0>(code, s), fp4_pair<1>(code, s), fp4_pair<2>(code, s),
-                   fp4_pair<3>(code, s));
+    if constexpr (MODE != 2) {
+      unsigned char* dst = block(dw[i], i);
+      store_codes<D>(dst, dw[i] & 15, c, v[i], code[i]);
+      if ((c & 31) == 0) dst[fp4_scale<D>(dw[i] & 15, c, v[i])] = (unsigned char)byte[i];
+    } else {
+      const float s = __builtin_bit_cast(float, byte[i] << 23);
+      __builtin_nontemporal_store(u32x4{fp4_pair<0>(code[i], s), fp4_pair<1>(code[i], s),
+                                        fp4_pair<2>(code[i], s), fp4_pair<3>(code[i], s)},
+                                  reinterpret_cast<u32x4*>((v[i] ? a.v_out : a.k_out) + row[i]));
+    }
   }
 }
 
@@ -157,7 +190,8 @@ void launch_fp4(const KvWriteArgs& a, unsigned grid, hipStream_t stream) {
 
 hipError_t launch_kv_write(const KvWriteArgs& a, hipStream_t stream) {
   const int64_t threads = (int64_t)a.n * a.Hkv * 2 * (a.fp4_dim ? a.fp4_dim / 8 : a.row_bytes / 16);
-  const int64_t grid = (threads + 255) / 256;
+  const int64_t block = a.fp4_dim ? 256 * kPieces : 256;
+  const int64_t grid = (threads + block - 1) / block;
   if (grid == 0) return hipSuccess;
   if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
   if (a.fp4_dim == 64) launch_fp4<64>(a, (unsigned)grid, stream);
