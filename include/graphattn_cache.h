@@ -41,7 +41,8 @@ ga_status graphattn_kv_read(const void* kv_page_pool, const int32_t* slot_words,
  *   mass_in   [num_pages x 16] device float32, or NULL (0); may be mass_out itself
  *   mass_out  [num_pages x 16] device float32; other slots are left as they were
  * One array may gather several layers (they share the slots): one call per layer, decay 1 but for the
- * first.  A row whose lse is infinite counts for nothing.  Sums are float32, and the same bits for the
+ * first.  A row whose lse is infinite counts for nothing; a token with a score that is NaN, or +infinite in
+ * such a row, has mass NaN.  Sums are float32, and the same bits for the
  * same inputs.  A plan without a current schedule is scheduled first.  GA_EINVAL where two segments on
  * paths own the same page (their slots would be written twice) and for a decay that is not finite.
  * Decode and multi-query plans, all pool types; asynchronous on hip_stream, and calls on one plan do not
@@ -54,7 +55,7 @@ ga_status graphattn_run_mass(ga_plan* plan, const void* q, const void* kv_page_p
  * keep_counts[s] of its seg_len[s] tokens: its first first_tokens and last recent_tokens tokens, then
  * those with the largest mass, ties to the lower position.  (-0 counts as 0; a NaN mass counts above
  * every number.)  GA_EINVAL unless min(seg_len[s], first_tokens + recent_tokens) <= keep_counts[s] <=
- * seg_len[s].
+ * seg_len[s]; GA_EUNSUPPORTED for a segment of more than 2^30 tokens.
  *
  * evict_create validates the table, copies it to the device and enqueues the upload on hip_stream (the
  * host arrays may be released on return; the handle serves any number of selections with these lengths

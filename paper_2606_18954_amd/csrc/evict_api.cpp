@@ -72,6 +72,9 @@ ga_status evict_create(const ga_segment_table* st, const int32_t* keep, int32_t 
   for (int32_t s = 0; s < S; ++s) {
     const int32_t len = st->seg_len[s];
     if (len < 1) return vfail(GA_EINVAL, "segment %d has length %d (< 1)", s, len);
+    // (positions run past a segment's end by less than a group of tokens)
+    if (len > (1 << 30))
+      return vfail(GA_EUNSUPPORTED, "segment %d has %d tokens (> 2^30)", s, len);
     const int64_t b = st->seg_page_offsets[s], e = st->seg_page_offsets[s + 1];
     if (e < b) return vfail(GA_EINVAL, "seg_page_offsets decreases at segment %d", s);
     const int64_t need = ((int64_t)len + ga::kPageTokens - 1) / ga::kPageTokens;

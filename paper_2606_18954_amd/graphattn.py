@@ -223,6 +223,14 @@ def _dev_ptr(t) -> int:
     return int(t.data_ptr())
 
 
+def _check_pool(pool, params: Params):
+    """An MXFP4 pool's bytes (uint8) hold its pages: a tensor of another layout would be read past its end."""
+    if params.dtype == GA_MXFP4 and (
+            pool.element_size() != 1 or
+            pool.numel() < 17 * params.head_dim * params.num_kv_heads * params.num_pages):
+        raise ValueError("an MXFP4 pool is a uint8 tensor [num_pages, Hkv, 17 D]")
+
+
 def decode(q, pool, graph: HostGraph, params: Params, out=None, lse=None, stream=None):
     """graphattn_decode on torch tensors: returns (out [B, Hq, D], lse [B, Hq] float32)."""
     import torch
@@ -233,6 +241,7 @@ def decode(q, pool, graph: HostGraph, params: Params, out=None, lse=None, stream
         out = torch.empty((B, params.num_q_heads, params.head_dim), dtype=odt, device=q.device)
     if lse is None:
         lse = torch.empty((B, params.num_q_heads), dtype=torch.float32, device=q.device)
+    _check_pool(pool, params)
     _check(lib.graphattn_decode(_dev_ptr(q), _dev_ptr(pool), ctypes.byref(graph.st),
                                 ctypes.byref(graph.bp), _dev_ptr(out), _dev_ptr(lse),
                                 ctypes.byref(params), _stream_handle(stream)))
@@ -243,6 +252,7 @@ def decode_static(q, pool, graph: HostGraph, params: Params, out, lse, stream=No
     """graphattn_decode_static: graphattn_decode with its workspace in the library's static
     device array (no allocation; the caller passes out and lse)."""
     lib = load_library()
+    _check_pool(pool, params)
     _check(lib.graphattn_decode_static(_dev_ptr(q), _dev_ptr(pool), ctypes.byref(graph.st),
                                        ctypes.byref(graph.bp), _dev_ptr(out), _dev_ptr(lse),
                                        ctypes.byref(params), _stream_handle(stream)))
@@ -268,6 +278,7 @@ def extend(q, pool, graph: HostGraph, query_counts, params: Params, out=None, ls
         out = torch.empty((R, params.num_q_heads, params.head_dim), dtype=odt, device=q.device)
     if lse is None:
         lse = torch.empty((R, params.num_q_heads), dtype=torch.float32, device=q.device)
+    _check_pool(pool, params)
     _check(lib.graphattn_extend(_dev_ptr(q), _dev_ptr(pool), ctypes.byref(graph.st),
                                 ctypes.byref(graph.bp), _ptr(cnt, ctypes.c_int32), _dev_ptr(out),
                                 _dev_ptr(lse), ctypes.byref(params), _stream_handle(stream)))
@@ -280,6 +291,7 @@ def kv_append(pool, k_new, v_new, slot_words, params: Params, stream=None):
     n = int(slot_words.numel())
     if k_new.shape[0] != n or v_new.shape[0] != n:
         raise ValueError("one K row and one V row per slot word")
+    _check_pool(pool, params)
     _check(lib.graphattn_kv_append(_dev_ptr(pool), _dev_ptr(k_new), _dev_ptr(v_new),
                                    _dev_ptr(slot_words), n, ctypes.byref(params),
                                    _stream_handle(stream)))
@@ -291,6 +303,7 @@ def kv_copy(pool, src_words, dst_words, params: Params, stream=None):
     n = int(dst_words.numel())
     if src_words.numel() != n:
         raise ValueError("one source word per destination word")
+    _check_pool(pool, params)
     _check(lib.graphattn_kv_copy(_dev_ptr(pool), _dev_ptr(src_words), _dev_ptr(dst_words), n,
                                  ctypes.byref(params), _stream_handle(stream)))
 
@@ -309,6 +322,9 @@ def kv_read(pool, slot_words, params: Params, k_out=None, v_out=None, stream=Non
         v_out = torch.zeros(shape, dtype=dt, device=pool.device)
     if tuple(k_out.shape) != shape or tuple(v_out.shape) != shape:
         raise ValueError("one K row and one V row [Hkv, D] per slot word")
+    if k_out.dtype != dt or v_out.dtype != dt or slot_words.dtype != torch.int32:
+        raise ValueError(f"k_out and v_out must be {dt}, slot_words int32")
+    _check_pool(pool, params)
     _check(lib.graphattn_kv_read(_dev_ptr(pool), _dev_ptr(slot_words), n, _dev_ptr(k_out),
                                  _dev_ptr(v_out), ctypes.byref(params), _stream_handle(stream)))
     return k_out, v_out
@@ -475,6 +491,8 @@ class Plan:
                 _ptr(self.query_counts, ctypes.c_int32), ctypes.byref(params),
                 _stream_handle(stream), ctypes.byref(h)))
         self.handle = h
+        # query rows of a run
+        self.rows = int(graph.bp.num_branches if query_counts is None else self.query_counts.sum())
 
     def set_lengths(self, seg_len, stream=None):
         """New segment lengths (host int32 [num_segments]); schedule again before the next run."""
@@ -489,15 +507,24 @@ class Plan:
         _check(self.lib.graphattn_schedule(self.handle, _stream_handle(stream)))
 
     def run(self, q, pool, out, lse, stream=None):
+        _check_pool(pool, self.params)
         _check(self.lib.graphattn_run(self.handle, _dev_ptr(q), _dev_ptr(pool), _dev_ptr(out),
                                       _dev_ptr(lse), _stream_handle(stream)))
 
     def run_mass(self, q, pool, lse, mass_out, mass_in=None, decay: float = 1.0, stream=None):
         """graphattn_run_mass: the attention weight every cached token received from these rows
         (lse as run() wrote it), added to decay x mass_in (float32 [num_pages x 16])."""
+        import torch
+        p = self.params
+        _check_pool(pool, p)
+        if q.numel() < self.rows * p.num_q_heads * p.head_dim or \
+                lse.numel() < self.rows * p.num_q_heads:
+            raise ValueError("one row of q and of lse per query")
         for t in (mass_out, mass_in):
-            if t is not None and t.numel() < 16 * self.params.num_pages:
+            if t is not None and t.numel() < 16 * p.num_pages:
                 raise ValueError("one mass per slot of the pool")
+        if any(t is not None and t.dtype != torch.float32 for t in (lse, mass_out, mass_in)):
+            raise ValueError("lse and the masses must be float32")
         _check(self.lib.graphattn_run_mass(self.handle, _dev_ptr(q), _dev_ptr(pool), _dev_ptr(lse),
                                            _dev_ptr(mass_in), float(decay), _dev_ptr(mass_out),
                                            _stream_handle(stream)))
@@ -584,14 +611,16 @@ class Evict:
     def select(self, mass, positions=None, slot_words=None, stream=None):
         """(positions, slot_words), int32 [total] each, from the mass of every slot."""
         import torch
-        if mass.numel() < 16 * self.num_pages:
-            raise ValueError("one mass per slot of the pool")
+        if mass.numel() < 16 * self.num_pages or mass.dtype != torch.float32:
+            raise ValueError("one mass per slot of the pool, float32")
         if positions is None:
             positions = torch.empty(self.total, dtype=torch.int32, device=mass.device)
         if slot_words is None:
             slot_words = torch.empty(self.total, dtype=torch.int32, device=mass.device)
         if positions.numel() < self.total or slot_words.numel() < self.total:
             raise ValueError("one position and one slot word per token that stays")
+        if positions.dtype != torch.int32 or slot_words.dtype != torch.int32:
+            raise ValueError("positions and slot_words must be int32")
         if self.total:
             _check(self.lib.graphattn_evict_select(self.handle, _dev_ptr(mass),
                                                    _dev_ptr(positions), _dev_ptr(slot_words),

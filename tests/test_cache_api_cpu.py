@@ -106,6 +106,7 @@ def test_evict_create_errors():
     assert _create(pages=[0, 1, 2, -3, 4, 5]) == G.GA_ERANGE
     assert _create(num_pages=-1) == G.GA_EINVAL
     assert _create(num_pages=(1 << 27) + 1) == G.GA_EUNSUPPORTED
+    assert _create(lens=((1 << 30) + 1,), keep=(1,), offsets=[0, 5], num_pages=1 << 27) == G.GA_EUNSUPPORTED
     h = ctypes.c_void_p()
     k = np.zeros(3, dtype=np.int32)
     kp = k.ctypes.data_as(ctypes.POINTER(ctypes.c_int32))
@@ -164,3 +165,22 @@ int main(void) {
                         "-Wl,-rpath," + lib, "-o", str(exe)], capture_output=True, text=True)
     assert r.returncode == 0, r.stderr
     assert subprocess.run([str(exe)]).returncode == 0
+
+
+def test_binding_refuses_tensors_of_other_types_and_sizes():
+    """(Before any pointer is taken: these are tensors of the host.)"""
+    torch = pytest.importorskip("torch")
+    p = G.make_params(4, 2, 64, 3, "mxfp4")
+    pool, words = G.empty_pool(p, "cpu"), torch.zeros(2, dtype=torch.int32)
+    kv = torch.zeros(2, 2, 64, dtype=torch.bfloat16)
+    for bad in (pool[:-1], torch.zeros(3, 2, 2, 16, 64, dtype=torch.bfloat16)):
+        for call in (lambda: G.kv_append(bad, kv, kv, words, p), lambda: G.kv_copy(bad, words, words, p),
+                     lambda: G.kv_read(bad, words, p, kv, kv)):
+            with pytest.raises(ValueError, match="MXFP4 pool"):
+                call()
+    with pytest.raises(ValueError, match="must be"):
+        G.kv_read(pool, words, p, kv.half(), kv)
+    with pytest.raises(ValueError, match="int32"):
+        G.kv_read(pool, words.long(), p, kv, kv)
+    with pytest.raises(ValueError, match="Hkv, D"):
+        G.kv_read(pool, words, p, kv[:1], kv)

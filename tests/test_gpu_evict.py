@@ -146,6 +146,12 @@ def test_mass_refusals():
             assert call(*a) == G.GA_EINVAL and G.last_error()
         with pytest.raises(ValueError):
             pl.run_mass(buf, buf, buf, torch.zeros(63, device="cuda"))
+        # (1 row of 4 heads x 64, 4 pages)
+        for q, lse, out, into in ((buf[:255], buf, buf[:64], None), (buf, buf[:3], buf[:64], None),
+                                  (buf, buf.double(), buf[:64], None), (buf, buf, buf[:64].double(), None),
+                                  (buf, buf, buf[:64], buf[:64].half())):
+            with pytest.raises(ValueError):
+                pl.run_mass(q, buf, lse, out, into)
 
 
 # ----------------------------------------------------------------------------------------------
@@ -174,6 +180,13 @@ def _masses(rng, kind, n):
         return rng.integers(0, 3, n).astype(np.float32)
     if kind == "equal":
         return np.full(n, 0.25, dtype=np.float32)
+    if kind == "mostly zero":
+        return np.where(rng.random(n) < 0.97, 0.0, rng.random(n)).astype(np.float32)
+    if kind == "uneven":                                 # a dense run of keys, far from a few others
+        x = (1 + 2.0 ** -23 * rng.integers(0, 5000, n)).astype(np.float32)
+        x[rng.random(n) < 0.02] = 1e-40
+        x[rng.random(n) < 0.02] = 1e38
+        return x
     x = rng.standard_normal(n).astype(np.float32)        # signs, zeros of both signs, NaN, infinities
     x[rng.random(n) < 0.2] = 0.0
     x[rng.random(n) < 0.2] = -0.0
@@ -184,7 +197,7 @@ def _masses(rng, kind, n):
     return x
 
 
-@pytest.mark.parametrize("kind", ["spread", "ties", "equal", "special"])
+@pytest.mark.parametrize("kind", ["spread", "ties", "equal", "special", "mostly zero", "uneven"])
 @pytest.mark.parametrize("lens", [[1], [2, 16, 17, 64, 65, 1023, 1024], [1025, 2048, 5],
                                   [16383, 16384, 1000], [16385, 40, 40000, 1500]])
 def test_select(lens, kind):
@@ -198,6 +211,29 @@ def test_select(lens, kind):
                                 (0, 0, n), (0, 0, 0 * n), (0, 0, np.minimum(n, 1)), (0, 0, n - 1),
                                 (3, 0, np.minimum(n, 3)), (0, 7, np.minimum(n, 7))):
         _check_select(mass, g, keep, first, recent)
+
+
+def test_two_selections_at_once():
+    """One handle, two streams and two masses: nothing is shared but the tables."""
+    require_gpu()
+    say("[case] two selections at once")
+    rng = np.random.default_rng(5)
+    lens = [700, 3000, 64, 20000, 1024]
+    g = W.assemble_graph(lens, [list(range(5))], 4)
+    mass = [_masses(rng, kind, 16 * g.num_pages) for kind in ("spread", "special")]
+    keep = [n // 2 for n in lens]
+    dev = [torch.from_numpy(m).cuda() for m in mass]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    with G.Evict(G.HostGraph.from_graph(g), keep, 2, 3, g.num_pages) as ev:
+        out = [[torch.zeros(ev.total, dtype=torch.int32, device="cuda") for _ in range(2)] for _ in dev]
+        torch.cuda.synchronize()
+        for _ in range(3):
+            for m, o, st in zip(dev, out, streams):
+                ev.select(m, *o, stream=st)
+        torch.cuda.synchronize()
+    for m, (p, w) in zip(mass, out):
+        rp, rw = C.evict_select(m, g.seg_len, g.seg_page_offsets, g.seg_pages, keep, 2, 3)
+        assert np.array_equal(p.cpu().numpy(), rp) and np.array_equal(w.cpu().numpy(), rw)
 
 
 def test_select_writes_only_its_outputs():
@@ -223,6 +259,10 @@ def test_select_writes_only_its_outputs():
                                           st) == G.GA_EINVAL
         with pytest.raises(ValueError):
             ev.select(mass[:-1].contiguous())
+        with pytest.raises(ValueError):
+            ev.select(mass.double())
+        with pytest.raises(ValueError):
+            ev.select(mass, torch.empty(720, dtype=torch.int64, device="cuda"))
         with pytest.raises(ValueError):
             ev.select(mass, torch.empty(719, dtype=torch.int32, device="cuda"))
         torch.cuda.synchronize()
