@@ -177,18 +177,24 @@ __global__ __launch_bounds__(kAttnThreads, FP4 ? fp4_wgs_per_cu(false) : mq_wgs_
                    __builtin_amdgcn_readfirstlane(dst + i * 1024));
   };
 
-  // MXFP4: this lane's share of the wave's eight tokens (w0 ..): D / 16 bytes of K codes (token w0 + lane / 8,
-  // D / 8 channels) and of V codes (slice (lane mod 32) / 2 of two tokens from w0 + 4 (lane / 32) + 2 (lane mod
-  // 2) on), each with a word of scales.
+  // MXFP4: this lane's share of the wave's eight tokens (w0 ..): D / 16 bytes of K codes (token kt, channels
+  // kc D / 8 on) and of V codes (two tokens from vt on, channels vr D / 16 on), each with a word of scales.
+  // Eight lanes write 128 bytes of a slot at a time, to different banks if their 16-byte chunks differ mod 8:
+  // so half of them take the K token four further (its chunks' lowest bit differs by the permutation), or the V
+  // channels four slices further.
   struct Raw {
     u32x2 c;
     unsigned s;
   };
   const int w0 = 8 * (wave & 1);
-  const unsigned kf_off = w0 * (D / 2) + lane * (D / 16);
-  const unsigned kf_byte = (w0 + lane / 8) * F::NS + (lane % 8) * (D / 8) / 32;
-  const unsigned vf_off = F::V + (w0 / 4) * 2 * D + lane * (D / 16);
-  const unsigned vf_scale = F::VS + ((w0 / 4 + lane / 32) * F::NS + (lane % 32) / 2 * F::SL / 32) * 4;
+  const int kt = w0 + (D == 128 ? 4 * (lane / 4 % 2) + lane / 16 : lane / 8);
+  const int kc = D == 128 ? lane % 4 + 4 * (lane / 8 % 2) : lane % 8;
+  const unsigned kf_off = kt * (D / 2) + kc * (D / 16);
+  const unsigned kf_byte = kt * F::NS + kc * (D / 8) / 32;
+  const int vt = w0 + 4 * (lane / 32) + 2 * (lane % 2);
+  const int vr = D == 128 ? (lane % 32 / 2) ^ (lane % 2 * 4) : lane % 32 / 2;
+  const unsigned vf_off = F::V + (vt / 4) * 2 * D + vr * (D / 8) + lane % 2 * (D / 16);
+  const unsigned vf_scale = F::VS + (vt / 4 * F::NS + vr * F::SL / 32) * 4;
   auto load_raw = [&](Raw& x, const unsigned char* base, unsigned off, unsigned scale) {
     const page_t page = page_at(base, F::PAGE);
     if constexpr (D == 128) x.c = load8(page, off);
@@ -206,32 +212,30 @@ __global__ __launch_bounds__(kAttnThreads, FP4 ? fp4_wgs_per_cu(false) : mq_wgs_
   typedef __attribute__((address_space(3))) u32x2 lds_u32x2;
   auto put_kf = [&](const Raw& x, int slot) {
     const float s = fp4_exp_at(x.s, 8 * (kf_byte & 3));
-    const int tok = w0 + lane / 8;
-    lds_uchar* row = slot_row(slot, tok);
+    lds_uchar* row = slot_row(slot, kt);
 #pragma unroll
     for (int i = 0; i < D / 64; ++i) {
       const unsigned w = x.c[i];
-      *(lds_u32x4*)(row + (((lane % 8 * (D / 64) + i) ^ fswz<D>(tok)) << 4)) =
+      *(lds_u32x4*)(row + (((kc * (D / 64) + i) ^ fswz<D>(kt)) << 4)) =
           u32x4{fp4_pair<0>(w, s), fp4_pair<1>(w, s), fp4_pair<2>(w, s), fp4_pair<3>(w, s)};
     }
   };
   // (a token past the page's valid ones may hold anything: its scale becomes the smallest, so that the
   // probability 0 meets a finite value)
   auto put_vf = [&](const Raw& x, int slot, int vm1) {
-    const int t0 = w0 + 4 * (lane / 32) + 2 * (lane % 2), r = (lane % 32) / 2;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const int tok = t0 + i;
+      const int tok = vt + i;
       const unsigned sw = tok <= vm1 ? x.s : 0;
       const float s = fp4_exp_at(sw, 16 * (lane % 2) + 8 * i);
       lds_uchar* row = slot_row(C::SLOTS + slot, tok);
       if constexpr (D == 128) {
         const unsigned w = x.c[i];
-        *(lds_u32x4*)(row + ((r ^ fswz<D>(tok)) << 4)) =
+        *(lds_u32x4*)(row + ((vr ^ fswz<D>(tok)) << 4)) =
             u32x4{fp4_pair<0>(w, s), fp4_pair<1>(w, s), fp4_pair<2>(w, s), fp4_pair<3>(w, s)};
       } else {
         const unsigned w = x.c[0];
-        *(lds_u32x2*)(row + (((r >> 1) ^ fswz<D>(tok)) << 4) + 8 * (r & 1)) =
+        *(lds_u32x2*)(row + (((vr >> 1) ^ fswz<D>(tok)) << 4) + 8 * (vr & 1)) =
             i == 0 ? u32x2{fp4_pair<0>(w, s), fp4_pair<1>(w, s)}
                    : u32x2{fp4_pair<2>(w, s), fp4_pair<3>(w, s)};
       }
