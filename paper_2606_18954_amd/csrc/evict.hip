@@ -23,8 +23,7 @@ namespace {
 
 __device__ __forceinline__ unsigned key_of(float x) {
   const unsigned b = __builtin_bit_cast(unsigned, x + 0.f);
-  if ((b & 0x7fffffffu) > 0x7f800000u) return 0xfffffffeu;
-  return b & 0x80000000u ? ~b : b | 0x80000000u;
+  return x != x ? 0xfffffffeu : b ^ ((unsigned)((int)b >> 31) | 0x80000000u);
 }
 
 // Words and keys of N tokens from t on, STEP apart (key 0, below every token's, past the segment's end: those
@@ -33,23 +32,30 @@ template <int N, int STEP>
 __device__ __forceinline__ void tokens(const EvictArgs& a, const EvictSeg& s, int t, int* word,
                                        unsigned* key) {
   float m[N];
+  const int32_t* pages = a.pages + s.pages;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const int u = min(t + STEP * i, s.len - 1);
-    word[i] = a.pages[s.pages + (u >> 4)] * kPageTokens + (u & 15);
+    const unsigned u = (unsigned)min(t + STEP * i, s.len - 1);
+    word[i] = pages[u >> 4] * kPageTokens + (int)(u & 15);
   }
 #pragma unroll
-  for (int i = 0; i < N; ++i) m[i] = a.mass[word[i]];
+  for (int i = 0; i < N; ++i) m[i] = a.mass[(unsigned)word[i]];
+#pragma unroll
+  for (int i = 0; i < N; ++i) key[i] = key_of(m[i]);
+  // (t - lane: uniform, the first of the wave's tokens)
+  const int t0 = __builtin_amdgcn_readfirstlane(t);
+  if (t0 >= a.first && t0 + STEP * (N - 1) + 63 < s.len - a.recent) return;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const int u = t + STEP * i;
-    key[i] = u < a.first || u >= s.len - a.recent ? 0xffffffffu : key_of(m[i]);
+    if (u < a.first || u >= s.len - a.recent) key[i] = 0xffffffffu;
     if (u >= s.len) key[i] = 0;
   }
 }
 
 __device__ __forceinline__ int below(uint64_t m, int lane) {
-  return __builtin_popcountll(m & ((1ull << lane) - 1));
+  (void)lane;
+  return (int)__builtin_amdgcn_mbcnt_hi((unsigned)(m >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)m, 0));
 }
 
 constexpr unsigned kZeroKey = 0x80000000u;           // of no mass, and of -0
@@ -118,14 +124,21 @@ __device__ __forceinline__ Bounds first_bounds(int n, int pos, unsigned kmin, un
 
 __device__ __forceinline__ bool positive_key(unsigned k) { return k > kZeroKey && k != 0xffffffffu; }
 
+// Least and largest of a wave's values, in every lane: exchanges within rows of 16 lanes, then between them.
 __device__ __forceinline__ void wave_min_max(unsigned& lo, unsigned& hi) {
-#pragma unroll
-  for (int d = 32; d; d /= 2) {
-    lo = min(lo, (unsigned)__shfl_xor((int)lo, d));
-    hi = max(hi, (unsigned)__shfl_xor((int)hi, d));
-  }
-  lo = __builtin_amdgcn_readfirstlane(lo);
-  hi = __builtin_amdgcn_readfirstlane(hi);
+  auto step = [&](auto f) {
+    lo = min(lo, f(lo));
+    hi = max(hi, f(hi));
+  };
+  step([](unsigned x) { return (unsigned)__builtin_amdgcn_mov_dpp((int)x, 0xB1, 0xf, 0xf, true); });   // lane ^ 1
+  step([](unsigned x) { return (unsigned)__builtin_amdgcn_mov_dpp((int)x, 0x4E, 0xf, 0xf, true); });   // lane ^ 2
+  step([](unsigned x) { return (unsigned)__builtin_amdgcn_mov_dpp((int)x, 0x141, 0xf, 0xf, true); });  // 7 - lane of 8
+  step([](unsigned x) { return (unsigned)__builtin_amdgcn_mov_dpp((int)x, 0x140, 0xf, 0xf, true); });  // 15 - lane of 16
+  const unsigned l = min(min((unsigned)__builtin_amdgcn_readlane((int)lo, 0), (unsigned)__builtin_amdgcn_readlane((int)lo, 16)),
+                         min((unsigned)__builtin_amdgcn_readlane((int)lo, 32), (unsigned)__builtin_amdgcn_readlane((int)lo, 48)));
+  hi = max(max((unsigned)__builtin_amdgcn_readlane((int)hi, 0), (unsigned)__builtin_amdgcn_readlane((int)hi, 16)),
+           max((unsigned)__builtin_amdgcn_readlane((int)hi, 32), (unsigned)__builtin_amdgcn_readlane((int)hi, 48)));
+  lo = l;
 }
 
 // LDS written by a wave's lanes, read by its others.
@@ -137,12 +150,10 @@ __device__ __forceinline__ void wave_sync() {
 __global__ __launch_bounds__(256) void k_evict_wave(EvictArgs a) {
   constexpr int NK = kEvictWave / 64, NB = 4;        // keys a lane, in runs of NB that a segment has or not
   __shared__ unsigned s_rest[4][64];                 // (each wave has its own: no barrier)
-  __shared__ int s_num[4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int id = (int)blockIdx.x * 4 + wave;
   if (id >= a.n_wave) return;
   s_rest[wave][lane] = 0;
-  if (lane == 0) s_num[wave] = 0;
   wave_sync();
   const EvictSeg s = a.segs[id];
   int word[NK];
@@ -183,10 +194,14 @@ __global__ __launch_bounds__(256) void k_evict_wave(EvictArgs a) {
       x.set(k, c, need);
     }
     if (!x.closed(need)) {
+      int at = 0;
       runs([&](int b) {
 #pragma unroll
-        for (int i = b; i < b + NB; ++i)
-          if (x.holds(key[i])) s_rest[wave][atomicAdd(&s_num[wave], 1)] = key[i];
+        for (int i = b; i < b + NB; ++i) {
+          const uint64_t in = __ballot(x.holds(key[i]));
+          if (x.holds(key[i])) s_rest[wave][at + below(in, lane)] = key[i];
+          at += __builtin_popcountll(in);
+        }
       });
       wave_sync();
       rank_rest(x, s_rest[wave][lane], need);
@@ -194,21 +209,26 @@ __global__ __launch_bounds__(256) void k_evict_wave(EvictArgs a) {
     T = x.clo == need ? x.lo - 1 : x.lo;
     ties = x.clo == need ? 0 : need - x.chi;
   }
-  int64_t out = s.out;
+  int32_t* positions = a.positions ? a.positions + s.out : nullptr;
+  int32_t* words = a.words ? a.words + s.out : nullptr;
+  unsigned out = 0;
   runs([&](int b) {
 #pragma unroll
     for (int i = b; i < b + NB; ++i) {
-      const bool eq = ties > 0 && key[i] == T;
-      const uint64_t me = __ballot(eq);
-      const bool stay = key[i] > T || (eq && below(me, lane) < ties);
-      ties -= min(ties, (int)__builtin_popcountll(me));
+      bool stay = key[i] > T;
+      if (ties > 0) {                                // (the same in every lane)
+        const bool eq = key[i] == T;
+        const uint64_t me = __ballot(eq);
+        stay = stay || (eq && below(me, lane) < ties);
+        ties -= min(ties, (int)__builtin_popcountll(me));
+      }
       const uint64_t ms = __ballot(stay);
       if (stay) {
-        const int64_t o = out + below(ms, lane);
-        if (a.positions) a.positions[o] = 64 * i + lane;
-        if (a.words) a.words[o] = word[i];
+        const unsigned o = out + (unsigned)below(ms, lane);
+        if (positions) positions[o] = 64 * i + lane;
+        if (words) words[o] = word[i];
       }
-      out += __builtin_popcountll(ms);
+      out += (unsigned)__builtin_popcountll(ms);
     }
   });
 }
@@ -232,7 +252,7 @@ __global__ __launch_bounds__(1024) void k_evict_group(EvictArgs a) {
     s_min = 0xffffffffu;
     s_max = 0;
   }
-  int word[NK] = {};
+  int word[NK];
   unsigned key[NK];
   auto runs = [&](int blk, auto f) {
 #pragma unroll
@@ -240,8 +260,6 @@ __global__ __launch_bounds__(1024) void k_evict_group(EvictArgs a) {
       if (blk * kEvictGroup + 1024 * b < s.len) f(b);
   };
   auto load = [&](int blk) {
-#pragma unroll
-    for (int i = 0; i < NK; ++i) key[i] = 0;
     runs(blk, [&](int b) {
       tokens<NB, 1024>(a, s, blk * kEvictGroup + 1024 * b + tid, word + b, key + b);
     });
@@ -297,14 +315,38 @@ __global__ __launch_bounds__(1024) void k_evict_group(EvictArgs a) {
     if (!x.closed(need)) {
       for (int blk = 0; blk < nblk; ++blk) {
         if (LONG) load(blk);
+        int c = 0;
         runs(blk, [&](int b) {
 #pragma unroll
-          for (int i = b; i < b + NB; ++i)
-            if (x.holds(key[i])) s_rest[atomicAdd(&s_num, 1)] = key[i];
+          for (int i = b; i < b + NB; ++i) c += __builtin_popcountll(__ballot(x.holds(key[i])));
+        });
+        if (c == 0) continue;
+        int at = 0;
+        if (lane == 0) at = atomicAdd(&s_num, c);
+        at = __builtin_amdgcn_readfirstlane(at);
+        runs(blk, [&](int b) {
+#pragma unroll
+          for (int i = b; i < b + NB; ++i) {
+            const uint64_t in = __ballot(x.holds(key[i]));
+            if (x.holds(key[i])) s_rest[at + below(in, lane)] = key[i];
+            at += __builtin_popcountll(in);
+          }
         });
       }
       __syncthreads();
-      rank_rest(x, s_rest[lane], need);
+      // (one wave: all sixteen would take four times as long)
+      if (wave == 0) {
+        rank_rest(x, s_rest[lane], need);
+        if (lane == 0) {
+          s_min = x.lo;
+          s_sum[0] = x.clo;
+          s_sum[1] = x.chi;
+        }
+      }
+      __syncthreads();
+      x.lo = __builtin_amdgcn_readfirstlane(s_min);
+      x.clo = __builtin_amdgcn_readfirstlane(s_sum[0]);
+      x.chi = __builtin_amdgcn_readfirstlane(s_sum[1]);
     }
     T = x.clo == need ? x.lo - 1 : x.lo;
     ties = x.clo == need ? 0 : need - x.chi;
@@ -314,12 +356,19 @@ __global__ __launch_bounds__(1024) void k_evict_group(EvictArgs a) {
     if (LONG) load(blk);
     // Per run of 64 tokens: keys above T and equal to it; then the running sums of both.
 #pragma unroll
-    for (int i = 0; i < NK; ++i) {
-      const int g = __builtin_popcountll(__ballot(key[i] > T));
-      const int e = __builtin_popcountll(__ballot(ties > 0 && key[i] == T));
-      if (lane == 0) {
-        s_gt[16 * i + wave] = g;
-        s_eq[16 * i + wave] = e;
+    for (int b = 0; b < NK; b += NB) {
+      const bool any = blk * kEvictGroup + 1024 * b < s.len;
+#pragma unroll
+      for (int i = b; i < b + NB; ++i) {
+        int g = 0, e = 0;
+        if (any) {
+          g = __builtin_popcountll(__ballot(key[i] > T));
+          if (ties > 0) e = __builtin_popcountll(__ballot(key[i] == T));
+        }
+        if (lane == 0) {
+          s_gt[16 * i + wave] = g;
+          s_eq[16 * i + wave] = e;
+        }
       }
     }
     __syncthreads();
@@ -354,19 +403,27 @@ __global__ __launch_bounds__(1024) void k_evict_group(EvictArgs a) {
       }
     }
     __syncthreads();
+    int32_t* positions = a.positions ? a.positions + out : nullptr;
+    int32_t* words = a.words ? a.words + out : nullptr;
+    runs(blk, [&](int b) {
 #pragma unroll
-    for (int i = 0; i < NK; ++i) {
-      const int pg = s_gt[16 * i + wave], pe = s_eq[16 * i + wave];
-      const bool eq = ties > 0 && key[i] == T;
-      const uint64_t me = __ballot(eq);
-      const bool stay = key[i] > T || (eq && pe + below(me, lane) < ties);
-      const uint64_t ms = __ballot(stay);
-      if (stay) {
-        const int64_t o = out + pg + min(pe, ties) + below(ms, lane);
-        if (a.positions) a.positions[o] = blk * kEvictGroup + 1024 * i + tid;
-        if (a.words) a.words[o] = word[i];
+      for (int i = b; i < b + NB; ++i) {
+        unsigned o = (unsigned)s_gt[16 * i + wave];
+        bool stay = key[i] > T;
+        if (ties > 0) {
+          const int pe = s_eq[16 * i + wave];
+          const bool eq = key[i] == T;
+          stay = stay || (eq && pe + below(__ballot(eq), lane) < ties);
+          o += (unsigned)min(pe, ties);
+        }
+        const uint64_t ms = __ballot(stay);
+        if (stay) {
+          o += (unsigned)below(ms, lane);
+          if (positions) positions[o] = blk * kEvictGroup + 1024 * i + tid;
+          if (words) words[o] = word[i];
+        }
       }
-    }
+    });
     const int tg = s_sum[0], te = min(s_sum[1], ties);
     out += tg + te;
     ties -= te;
