@@ -773,7 +773,10 @@ ga_status do_schedule(ga_plan* pl, hipStream_t stream) {
 
 // Attention workgroups of a plan's persistent grid on a device of num_cus CUs.
 int attn_grid(const ga_plan* pl, int num_cus) {
-  if (pl->p.dtype == GA_MXFP4) return num_cus * ga::fp4_wgs_per_cu(pl->z.few_rows);
+  if (pl->p.dtype == GA_MXFP4)
+    return num_cus * (pl->causal && !pl->z.few_pages
+                          ? ga::kMqFp4WgsPerCu
+                          : ga::fp4_wgs_per_cu(pl->z.few_rows, pl->p.head_dim));
   return ga::seg_attn_grid(pl->p.head_dim, pl->p.dtype == GA_BF16, pl->causal, pl->z.few_pages,
                            num_cus);
 }

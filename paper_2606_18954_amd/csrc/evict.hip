@@ -16,6 +16,11 @@
 // Segments of up to kEvictWave tokens: one wave each, keys and words in registers, no barrier.  Up to
 // kEvictGroup: one workgroup of 1024 threads, a barrier a step.  Longer ones: the same, but the keys are
 // read again for every step.
+//
+// What bounds it: latency.  3266 segments of 64 to 1024 tokens (1.8 M tokens, 14 MB), half of them kept: 11 to 14
+// us, half of it the three dependent loads (segment, page word, mass) of each wave; 256 segments of 8192: 14 to
+// 15 us, one workgroup per CU with a barrier a step.  The bytes would take 2.8 and 2.4 us.  Bit by bit, and one token's loads after another's, they
+// took 15.4 and 20.2.
 #include "evict_internal.hpp"
 
 namespace ga {
@@ -127,18 +132,21 @@ __device__ __forceinline__ bool positive_key(unsigned k) { return k > kZeroKey &
 // Least and largest of a wave's values, in every lane: exchanges within rows of 16 lanes, then between them.
 __device__ __forceinline__ void wave_min_max(unsigned& lo, unsigned& hi) {
   auto step = [&](auto f) {
-    lo = min(lo, f(lo));
-    hi = max(hi, f(hi));
+    lo = min(lo, (unsigned)f((int)lo));
+    hi = max(hi, (unsigned)f((int)hi));
   };
-  step([](unsigned x) { return (unsigned)__builtin_amdgcn_mov_dpp((int)x, 0xB1, 0xf, 0xf, true); });   // lane ^ 1
-  step([](unsigned x) { return (unsigned)__builtin_amdgcn_mov_dpp((int)x, 0x4E, 0xf, 0xf, true); });   // lane ^ 2
-  step([](unsigned x) { return (unsigned)__builtin_amdgcn_mov_dpp((int)x, 0x141, 0xf, 0xf, true); });  // 7 - lane of 8
-  step([](unsigned x) { return (unsigned)__builtin_amdgcn_mov_dpp((int)x, 0x140, 0xf, 0xf, true); });  // 15 - lane of 16
-  const unsigned l = min(min((unsigned)__builtin_amdgcn_readlane((int)lo, 0), (unsigned)__builtin_amdgcn_readlane((int)lo, 16)),
-                         min((unsigned)__builtin_amdgcn_readlane((int)lo, 32), (unsigned)__builtin_amdgcn_readlane((int)lo, 48)));
-  hi = max(max((unsigned)__builtin_amdgcn_readlane((int)hi, 0), (unsigned)__builtin_amdgcn_readlane((int)hi, 16)),
-           max((unsigned)__builtin_amdgcn_readlane((int)hi, 32), (unsigned)__builtin_amdgcn_readlane((int)hi, 48)));
+  step([](int x) { return __builtin_amdgcn_mov_dpp(x, 0xB1, 0xf, 0xf, true); });    // lane ^ 1
+  step([](int x) { return __builtin_amdgcn_mov_dpp(x, 0x4E, 0xf, 0xf, true); });    // lane ^ 2
+  step([](int x) { return __builtin_amdgcn_mov_dpp(x, 0x141, 0xf, 0xf, true); });   // 7 - lane, of 8
+  step([](int x) { return __builtin_amdgcn_mov_dpp(x, 0x140, 0xf, 0xf, true); });   // 15 - lane, of 16
+  unsigned l = 0xffffffffu, h = 0;
+#pragma unroll
+  for (int row = 0; row < 64; row += 16) {
+    l = min(l, (unsigned)__builtin_amdgcn_readlane((int)lo, row));
+    h = max(h, (unsigned)__builtin_amdgcn_readlane((int)hi, row));
+  }
   lo = l;
+  hi = h;
 }
 
 // LDS written by a wave's lanes, read by its others.

@@ -1,4 +1,4 @@
-// Segment attention over MXFP4 pools (decode and multi-query): one work item = (segment chain, page
+// Segment attention over MXFP4 pools (decode, and multi-query steps with few rows a page): one work item = (segment chain, page
 // chunk, row block of up to 128 query rows, kv-head), as in seg_attn.hip, with the work list, the
 // descriptors, the partial rows and the merge shared with it.
 //
@@ -24,6 +24,16 @@
 //
 // Online softmax as in seg_attn.hip (log2 domain, lazily moved reference), float32 throughout;
 // probabilities are rounded to bf16 for the second product (V's exponents need bf16's range).
+//
+// What bounds it.  Decode of 64 merged graphs, 1024 branches of 28/4 heads x 128 (449 K pages of a head, 0.98 GB):
+// 237 us, 4.6 TB/s of reads and writes where pages alone, read in this pattern, come at 5.9; the vector unit is
+// busy 58% of the time and the matrix cores 15%.  With the pages in the L2 the same instructions take 161 to
+// 172 us, and reading the pages without them 165: neither is hidden whole by the other.  256 branches of
+// 16384 tokens, 40/8 heads: 390 us, 4.7 TB/s.  16 step trees (38 MB): 18 us, one or two units a workgroup.
+// Rejected, on the first of these (246 us then): four waves per SIMD, no change; two kv-heads a unit, no
+// change, four slower (uneven ends); a unit's first pages loaded before the last one's rows are joined, no
+// change; page loads that skip the last turns' duplicates, 259 us and spills; three pairs of pages in flight,
+// slower.
 #include "attn_dev.hpp"
 #include "ga_internal.hpp"
 #include "mxfp4.hpp"
@@ -75,9 +85,13 @@ __device__ __forceinline__ float quad_sum(float v) {
   return v + __shfl_xor(v, 32);
 }
 
-// MAXNT: row tiles of a wave, one (steps with few rows a page) or two.
+// MAXNT: row tiles of a wave, one (steps with few rows a page: fewer registers, a workgroup more per CU) or two
+// (a page is converted for twice the rows).  The line is 32 rows a page (us, two | one): merged graphs of 1024
+// branches (16 rows) 258 | 250, 16 step trees (17 rows) 26.6 | 23.0, 30 prompts of 400 tokens with 10 branches of
+// 28/4 heads (40 rows) 60.5 | 60.1, with 20 branches (75 rows) 80 | 86; against the rule only the long contexts
+// above (12 rows, a fifth of the pages with 40), 390 | 402.
 template <int D, bool CAUSAL, int MAXNT>
-__global__ __launch_bounds__(kAttnThreads, fp4_wgs_per_cu(MAXNT == 1)) void k_fp4_attn(AttnArgs a) {
+__global__ __launch_bounds__(kAttnThreads, fp4_wgs_per_cu(MAXNT == 1, D)) void k_fp4_attn(AttnArgs a) {
   using C = QCfg<D>;
   using F = Fp4<D>;
   constexpr int PF = MAXNT == 1 ? 2 : 3;            // pairs of pages in flight or in use per wave

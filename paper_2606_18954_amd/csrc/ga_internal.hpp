@@ -15,8 +15,12 @@ constexpr int kRowsPerBlock = 128;
 // Upper bound on pages per work item (the chunk's page ids are staged in LDS).
 constexpr int kMaxChunkPages = 128;
 constexpr int kAttnThreads = 256;        // 4 wave64 per workgroup
-// Attention workgroups per CU over an MXFP4 pool, by registers (fp4_attn.hip; mq_attn.hip has many rows).
-__host__ __device__ constexpr int fp4_wgs_per_cu(bool few_rows) { return few_rows ? 3 : 2; }
+// Attention workgroups per CU over an MXFP4 pool, by registers: fp4_attn.hip (head_dim 128: 137 and 251; 64: 101
+// and 167) and mq_attn.hip (256 and 186).
+__host__ __device__ constexpr int fp4_wgs_per_cu(bool few_rows, int head_dim) {
+  return (few_rows ? 3 : 2) + (head_dim == 64 ? 1 : 0);
+}
+constexpr int kMqFp4WgsPerCu = 2;
 
 // Work-item descriptor (int32 words, one per item, fixed stride), written by the scheduler and
 // copied whole into LDS by the attention kernel:

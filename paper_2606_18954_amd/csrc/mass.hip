@@ -7,13 +7,21 @@
 // and all kv-heads owns those slots: no atomics, one order of the sums, the same bits every time.  Its
 // waves take different kv-heads first, and different pages where heads are few.
 //   S = Q K^T (16 rows x 16 tokens per matrix tile), p = 2^(S scale log2 e - lse log2 e)
-// A lane holds four rows' scores of one token, so a token's sum is three additions in the lane; the
-// four lanes of a token meet in LDS, with the kv-heads, once per unit.
+// A lane holds four rows' scores of one token, so a token's sum is three additions in the lane and two
+// exchanges with the other lanes of the token; the kv-heads' sums meet in LDS.
 //
 // Few rows (up to kMassRows, most chains of a decode step): two tiles' queries stay in registers and
 // the pages stream past, several of them on their way, once per two tiles (from the caches after the first
 // time).  More rows (prefill): a few pages stay, as matrix operands, and the rows stream past, one tile's
 // queries and the next one's row numbers on their way.
+//
+// What bounds it: reading K.  1024 branches of merged graphs, 28/4 heads x 128, MXFP4: 129 us, 0.65 GB read at
+// 5.0 TB/s (0.50 GB of them once; the rest are scales' half lines, queries and last pages read again), vector
+// unit busy 39%, matrix cores 13%.  16 step trees, bf16 (70 MB): 27 us, a chain of five dependent loads (chain,
+// page words and branches, queries and pages) and few pages a workgroup.  Measured and not taken: non-temporal
+// page loads (trees 28 -> 45 us: chains of more than two tiles read their pages again), three or six pages
+// on their way in place of four (135.0 and 138.8 against 134.5 us), workgroups of at most 32 or 64 pages x pairs
+// (no change), twice the workgroups (147 us).
 #include "attn_dev.hpp"
 #include "evict_internal.hpp"
 #include "mxfp4.hpp"

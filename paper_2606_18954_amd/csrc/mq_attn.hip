@@ -79,7 +79,7 @@ __device__ __forceinline__ int fswz(int tok) {
 //   whose waves convert every page for their own rows, takes 1.82 and bf16 pools 1.58 on that card.
 //   Prefill as above: 0.70 ms (0.84 PFLOP/s), fp4_attn.hip 0.87, bf16 pools 0.68.
 template <int D, bool FP4>
-__global__ __launch_bounds__(kAttnThreads, FP4 ? fp4_wgs_per_cu(false) : mq_wgs_per_cu(D)) void k_mq_attn(AttnArgs a) {
+__global__ __launch_bounds__(kAttnThreads, FP4 ? kMqFp4WgsPerCu : mq_wgs_per_cu(D)) void k_mq_attn(AttnArgs a) {
   using C = MCfg<D>;
   using F = Fp4<D>;
   constexpr int HEAD = FP4 ? F::PAGE : 2 * C::KVB;  // bytes of a page of one kv-head
