@@ -45,7 +45,8 @@ EQ_COUNTERS_MD = os.path.join(ROOT, "profiles", "equiv_classes_counters.md")
 CSRC = os.path.join(ROOT, "paper_2606_18954_amd", "csrc")
 # The sources whose change makes a kernel's committed counters stale: its own and its headers.
 KERNEL_SRCS = ("seg_attn.hip", "attn_dev.hpp", "ga_internal.hpp")
-EXT_KERNEL_SRCS = ("mq_attn.hip", "attn_dev.hpp", "ga_internal.hpp")
+EXT_KERNEL_SRCS = ("mq_attn.hip", "mq_attn.hpp", "attn_dev.hpp", "ga_internal.hpp", "mxfp4.hpp",
+                   "pool_load.hpp")
 EQ_KERNEL_SRCS = ("equiv.hip", "equiv_tiles.hpp", "attn_dev.hpp", "ga_internal.hpp")
 
 

@@ -14,8 +14,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libgraphattn.so")
-SOURCES = ["api.cpp", "sched.hip", "seg_attn.hip", "mq_attn.hip", "fp4_attn.hip",
-           "merge.hip", "kv_write.hip",
+SOURCES = ["api.cpp", "sched.hip", "seg_attn.hip", "mq_attn.hip", "mq_fp4_attn.hip",
+           "fp4_attn.hip", "merge.hip", "kv_write.hip",
            "equiv.hip", "equiv_api.cpp", "reward.hip",
            "mass.hip", "evict.hip", "evict_api.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -346,7 +346,7 @@ void size_schedule(const ga_segment_table* st, const ga_branch_paths* bp, const 
   // chunks also mean fewer partial rows to merge and fewer items to schedule.
   const int64_t wgs = 2LL * num_cus;
   const int64_t target_items = 4 * wgs;
-  // Multi-query plans whose pages are read for many rows run mq_attn.hip, whose four waves each own
+  // Multi-query plans whose pages are read for many rows run mq_attn.hpp, whose four waves each own
   // 32 rows of a block.  Its units are sized by the pages of every row block (each is a unit), and
   // not cut below 16 pages, so that short prompts keep one partial per row and need no merge.  The
   // lines lie where the two kernels cross (us per step, other kernel | mq_attn): 16 step trees of

@@ -1,4 +1,4 @@
-// Device helpers shared by the attention kernels (seg_attn.hip, mq_attn.hip) and the similarity kernels
+// Device helpers shared by the attention kernels (seg_attn.hip, mq_attn.hpp) and the similarity kernels
 // (equiv.hip): direct-to-LDS copies, partial-row stores, explicit waits and barriers.
 #pragma once
 
@@ -6,12 +6,14 @@
 
 namespace ga {
 
-// Multi-query attention of bf16 and MXFP4 plans with many query rows (mq_attn.hip): as many workgroups per
+// Multi-query attention of bf16 and MXFP4 plans with many query rows (mq_attn.hpp): as many workgroups per
 // CU as its registers allow (bf16, head_dim 128: 242, two waves per SIMD; 64: 165, three; MXFP4: 256 and
 // 186, two).
 __host__ __device__ constexpr int mq_wgs_per_cu(int head_dim) { return head_dim == 64 ? 3 : 2; }
 hipError_t launch_mq_attn(const AttnArgs& a, int head_dim, int grid, hipStream_t stream,
                           hipEvent_t t0, hipEvent_t t1);
+hipError_t launch_mq_fp4_attn(const AttnArgs& a, int head_dim, int grid, hipStream_t stream,
+                              hipEvent_t t0, hipEvent_t t1);
 // Attention over MXFP4 pools otherwise (fp4_attn.hip).
 hipError_t launch_fp4_attn(const AttnArgs& a, int head_dim, bool causal, int grid,
                            hipStream_t stream, hipEvent_t t0, hipEvent_t t1);

@@ -16,7 +16,7 @@ constexpr int kRowsPerBlock = 128;
 constexpr int kMaxChunkPages = 128;
 constexpr int kAttnThreads = 256;        // 4 wave64 per workgroup
 // Attention workgroups per CU over an MXFP4 pool, by registers: fp4_attn.hip (head_dim 128: 137 and 251; 64: 101
-// and 167) and mq_attn.hip (256 and 186).
+// and 167) and mq_attn.hpp (256 and 186).
 __host__ __device__ constexpr int fp4_wgs_per_cu(bool few_rows, int head_dim) {
   return (few_rows ? 3 : 2) + (head_dim == 64 ? 1 : 0);
 }
@@ -246,7 +246,7 @@ hipError_t launch_schedule(const DevGraph& g, const DevSchedule& sc, int32_t gro
                            int32_t chunk_pages, int64_t max_items, bool reuse,
                            hipStream_t stream);
 // few_pages: a decode step with under 64 pages (times kv-heads) per workgroup at two per CU, or a
-// multi-query step with few query rows per page (bf16 and MXFP4 steps with many run mq_attn.hip).
+// multi-query step with few query rows per page (bf16 and MXFP4 steps with many run mq_attn.hpp).
 // t0 / t1 (optional, timing events): bound to the kernel's own dispatch (hipExtLaunchKernel), so
 // that their elapsed time is the kernel's execution, without the queue's gaps around it.
 hipError_t launch_seg_attn(const AttnArgs& a, int head_dim, bool bf16, bool causal,

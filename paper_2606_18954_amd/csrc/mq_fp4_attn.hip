@@ -1,0 +1,13 @@
+// Multi-query attention over MXFP4 pools with many query rows a page.
+#include "mq_attn.hpp"
+
+namespace ga {
+
+hipError_t launch_mq_fp4_attn(const AttnArgs& a, int head_dim, int grid, hipStream_t stream,
+                              hipEvent_t t0, hipEvent_t t1) {
+  if (head_dim == 64) return launch_mq<64, true>(a, grid, stream, t0, t1);
+  if (head_dim == 128) return launch_mq<128, true>(a, grid, stream, t0, t1);
+  return hipErrorInvalidValue;
+}
+
+}  // namespace ga

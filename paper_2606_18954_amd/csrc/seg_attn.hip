@@ -53,7 +53,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
 // Workgroups per CU and ring depth: two workgroups with four stages for decode; the bf16
-// multi-query variant (steps with few query rows per page; mq_attn.hip takes the others) runs
+// multi-query variant (steps with few query rows per page; mq_attn.hpp takes the others) runs
 // three workgroups per CU with three stages each, and so does bf16 decode on a step with few
 // pages per workgroup (each workgroup then has one or two units, whose fixed costs more
 // workgroups overlap better).  (The fp32 variants keep
@@ -737,7 +737,9 @@ int seg_attn_grid(int head_dim, bool bf16, bool causal, bool few_pages, int num_
 hipError_t launch_seg_attn(const AttnArgs& a, int head_dim, bool bf16, bool causal,
                            bool few_pages, int grid, hipStream_t stream, hipEvent_t t0,
                            hipEvent_t t1) {
-  if (a.fp4 && (few_pages || !causal)) return launch_fp4_attn(a, head_dim, causal, grid, stream, t0, t1);
+  if (a.fp4)
+    return few_pages || !causal ? launch_fp4_attn(a, head_dim, causal, grid, stream, t0, t1)
+                                : launch_mq_fp4_attn(a, head_dim, grid, stream, t0, t1);
   if (bf16 && causal && !few_pages) return launch_mq_attn(a, head_dim, grid, stream, t0, t1);
   if (bf16) {
     if (head_dim == 64) return launch_t<64, true>(a, causal, few_pages, grid, stream, t0, t1);

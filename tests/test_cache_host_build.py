@@ -46,7 +46,7 @@ def _assembly(name, tmp_path):
 
 
 @needs_hipcc
-@pytest.mark.parametrize("name,kernels", [("fp4_attn.hip", 4), ("mq_attn.hip", 4), ("mass.hip", 6), ("evict.hip", 3)])
+@pytest.mark.parametrize("name,kernels", [("fp4_attn.hip", 4), ("mq_fp4_attn.hip", 2), ("mass.hip", 6), ("evict.hip", 3)])
 def test_kernels_keep_to_their_registers(name, kernels, tmp_path):
     text = _assembly(name, tmp_path)
     sizes = re.findall(r"; ScratchSize: (\d+)", text)
