@@ -405,3 +405,163 @@ def test_captured_cycle_replays():
     for s in (a, b):
         s.plan.close()
         s.ev.close()
+
+
+def test_pages_beyond_four_gigabytes():
+    """Every call on pages at the end of a pool of 4.1 GiB: byte offsets that pass 32 bits."""
+    require_gpu()
+    say("[case] pages beyond 4 GiB")
+    rng = np.random.default_rng(17)
+    Hq, Hkv, D = 16, 8, 128
+    lens, paths = W.with_new_steps([150, 37], [[0], [0, 1], [0]], [20, 33, 16])
+    g = W.assemble_graph(lens, paths, 6, slack_pages=4)
+    n = g.num_pages
+    P = 2 ** 32 // (Hkv * 17 * D) + 3 * n
+    assert (P - n) * Hkv * 17 * D > 2 ** 32
+    far = G.HostGraph(g.seg_len, g.seg_page_offsets, g.seg_pages + (P - n), g.path_offsets, g.path_segs)
+    p = G.make_params(Hq, Hkv, D, P, "mxfp4")
+    pool = torch.zeros(P, Hkv, 17 * D, dtype=torch.uint8, device="cuda")
+    raw = poison_unused(random_pool(rng, n, Hkv, D, -2, 1), g)
+    pool[-n:] = torch.from_numpy(raw).cuda()
+    # append and read: the last segment's tokens again
+    s = len(lens) - 1
+    words = np.array([int(g.seg_pages[g.seg_page_offsets[s] + t // 16]) * 16 + t % 16 for t in range(lens[s])])
+    kv = draw_q(rng, 2 * lens[s], Hkv, D)
+    k, v = kv[:lens[s]].contiguous(), kv[lens[s]:].contiguous()
+    dev_words = torch.from_numpy(words + 16 * (P - n)).int().cuda()
+    G.kv_append(pool, k.cuda(), v.cuda(), dev_words, p)
+    raw = C.append(raw, bits_of(k), bits_of(v), words)
+    assert np.array_equal(pool[-n:].cpu().numpy(), raw)
+    vals = C.pool_values(raw)
+    rk, rv = G.kv_read(pool, dev_words, p)
+    torch.cuda.synchronize()
+    assert np.array_equal(bits_of(rk), vals[words // 16, :, 0, words % 16])
+    assert np.array_equal(bits_of(rv), vals[words // 16, :, 1, words % 16])
+    for counts in (None, [20, 33, 16], [1, 2, 1]):
+        rows = 3 if counts is None else sum(counts)
+        q = draw_q(rng, rows, Hq, D)
+        out = torch.zeros(rows, Hq, D, dtype=torch.bfloat16, device="cuda")
+        lse = torch.zeros(rows, Hq, device="cuda")
+        mass = torch.full((16 * P,), -3.0, device="cuda")
+        with G.Plan(far, p, query_counts=counts) as pl:
+            pl.run(q.cuda(), pool, out, lse)
+            check_attention(f"far pages {counts}", out, lse, q, vals, g, Hq, Hkv, counts)
+            pl.run_mass(q.cuda(), pool, lse, mass)
+            torch.cuda.synchronize()
+        zero = np.zeros(16 * n, dtype=np.float32)
+        l64 = bits_of(lse).astype(float)
+        ref = C.mass(bits_of(q), vals, g, l64, Hq, Hkv, zero, 1.0, counts)
+        live = np.isfinite(ref)
+        off = np.abs(bits_of(mass[-16 * n:]) - ref)[live] / mass_bound(q, vals, g, l64, Hq, Hkv, ref, 0.0, zero,
+                                                                       counts)[live]
+        assert off.max() <= 1.0, counts
+        assert (mass[:-16 * n] == -3).all() and (bits_of(mass[-16 * n:])[~live] == -3).all()
+    # copy: to the first page (its codes and scales are the source's)
+    G.kv_copy(pool, dev_words[:16].contiguous(), torch.arange(16, dtype=torch.int32, device="cuda"), p)
+    ck, cv = G.kv_read(pool, torch.arange(16, dtype=torch.int32, device="cuda"), p)
+    torch.cuda.synchronize()
+    assert torch.equal(ck, rk[:16]) and torch.equal(cv, rv[:16])
+
+
+def test_select_on_the_highest_pages():
+    """Slot words up to 2^31 - 1, whose masses lie 8 GiB into their array."""
+    require_gpu()
+    say("[case] select on the highest pages")
+    rng = np.random.default_rng(23)
+    lens = [900, 3000, 17000, 64]
+    g = W.assemble_graph(lens, [[0, 1, 2, 3]], 4)
+    n, P = g.num_pages, 2 ** 27
+    mass = _masses(rng, "spread", 16 * n)
+    dev = torch.zeros(16 * P, device="cuda")
+    dev[-16 * n:] = torch.from_numpy(mass).cuda()
+    keep = [m // 3 for m in lens]
+    far = G.HostGraph(g.seg_len, g.seg_page_offsets, g.seg_pages + (P - n), g.path_offsets, g.path_segs)
+    with G.Evict(far, keep, 2, 5, P) as ev:
+        pos, words = ev.select(dev)
+        torch.cuda.synchronize()
+    rp, rw = C.evict_select(mass, g.seg_len, g.seg_page_offsets, g.seg_pages, keep, 2, 5)
+    assert np.array_equal(pos.cpu().numpy(), rp)
+    assert np.array_equal(words.cpu().numpy(), rw + 16 * (P - n))
+
+
+def test_mass_after_new_lengths():
+    """A plan that grew gives a fresh plan's mass, bit for bit where the parts are the same and within the
+    bound otherwise; slots past the shorter lengths are left as they were."""
+    require_gpu()
+    say("[case] mass after new lengths")
+    rng = np.random.default_rng(29)
+    Hq, Hkv, D = 8, 2, 64
+    final = W.assemble_graph([700, 90, 130], [[0, 1], [0, 2], [0]], 6, slack_pages=2)
+    pool, vals = _pool(rng, final, Hkv, D, "mxfp4")
+    p = G.make_params(Hq, Hkv, D, final.num_pages, "mxfp4")
+    q = draw_q(rng, 3, Hq, D)
+    with G.Plan(G.HostGraph([5, 1, 17], final.seg_page_offsets, final.seg_pages, final.path_offsets,
+                            final.path_segs), p) as pl:
+        for lens in ([5, 1, 17], [300, 33, 130], [700, 90, 130]):
+            pl.set_lengths(lens)
+            g = W.RolloutGraph(np.array(lens, dtype=np.int32), final.seg_page_offsets, final.seg_pages,
+                               final.path_offsets, final.path_segs, final.num_pages)
+            lse = C.attention(bits_of(q), vals, g, Hq, Hkv)[1].astype(np.float32)
+            out = torch.full((16 * g.num_pages,), -5.0, device="cuda")
+            pl.run_mass(q.cuda(), pool, torch.from_numpy(lse).cuda(), out)
+            torch.cuda.synchronize()
+            zero = np.zeros(16 * g.num_pages, dtype=np.float32)
+            ref = C.mass(bits_of(q), vals, g, lse.astype(float), Hq, Hkv, zero, 1.0)
+            live = np.isfinite(ref)
+            off = np.abs(bits_of(out) - ref)[live] / mass_bound(q, vals, g, lse, Hq, Hkv, ref, 0.0, zero)[live]
+            assert off.max() <= 1.0, lens
+            assert (bits_of(out)[~live] == -5).all(), lens
+
+
+def test_captured_extend_replays():
+    """append, attention of many query rows and mass, captured: every replay equals the eager calls."""
+    require_gpu()
+    say("[case] captured extend")
+    rng = np.random.default_rng(37)
+    Hq, Hkv, D = 28, 4, 128
+    counts = [40, 25, 33]
+    lens, paths = W.with_new_steps([300, 20], [[0], [0, 1], [0]], counts)
+    g = W.assemble_graph(lens, paths, 6, slack_pages=1)
+    start = torch.from_numpy(random_pool(rng, g.num_pages, Hkv, D, -2, 1)).cuda()
+    p = G.make_params(Hq, Hkv, D, g.num_pages, "mxfp4")
+    rows = sum(counts)
+    words = torch.from_numpy(np.concatenate([
+        g.seg_pages[g.seg_page_offsets[s] + np.arange(lens[s]) // 16].astype(np.int32) * 16 +
+        np.arange(lens[s], dtype=np.int32) % 16 for s in range(2, 5)])).cuda()
+
+    class Set:
+        def __init__(self):
+            self.q = torch.zeros(rows, Hq, D, dtype=torch.bfloat16, device="cuda")
+            self.kv = torch.zeros(2, len(words), Hkv, D, dtype=torch.bfloat16, device="cuda")
+            self.pool, self.out = start.clone(), torch.zeros_like(self.q)
+            self.lse = torch.zeros(rows, Hq, device="cuda")
+            self.mass = torch.zeros(16 * g.num_pages, device="cuda")
+            self.plan = G.Plan(G.HostGraph.from_graph(g), p, query_counts=counts)
+            self.plan.schedule()
+
+        def run(self):
+            G.kv_append(self.pool, self.kv[0], self.kv[1], words, p)
+            self.plan.run(self.q, self.pool, self.out, self.lse)
+            self.plan.run_mass(self.q, self.pool, self.lse, self.mass, self.mass, 0.5)
+
+    a, b = Set(), Set()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        a.run()
+    torch.cuda.synchronize()
+    for i in range(4):
+        q, kv = draw_q(rng, rows, Hq, D).cuda(), draw_q(rng, 2 * len(words), Hkv, D).cuda().view_as(a.kv)
+        for x in (a, b):
+            x.q.copy_(q)
+            x.kv.copy_(kv)
+        torch.cuda.synchronize()
+        graph.replay()
+        b.run()
+        torch.cuda.synchronize()
+        for name in ("pool", "mass", "lse"):
+            assert torch.equal(getattr(a, name), getattr(b, name)), (i, name)
+        assert torch.equal(a.out.view(torch.int16), b.out.view(torch.int16)), i
+    for x in (a, b):
+        x.plan.close()
