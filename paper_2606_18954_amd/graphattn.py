@@ -223,12 +223,18 @@ def _dev_ptr(t) -> int:
     return int(t.data_ptr())
 
 
-def _check_pool(pool, params: Params):
-    """An MXFP4 pool's bytes (uint8) hold its pages: a tensor of another layout would be read past its end."""
-    if params.dtype == GA_MXFP4 and (
-            pool.element_size() != 1 or
-            pool.numel() < 17 * params.head_dim * params.num_kv_heads * params.num_pages):
+def _check_pool(pool, params: Params, *rows):
+    """An MXFP4 pool's bytes (uint8) hold its pages, and q, K and V rows beside it are bf16: tensors of another
+    layout would be read past their end."""
+    if params.dtype != GA_MXFP4:
+        return
+    if pool.element_size() != 1 or \
+            pool.numel() < 17 * params.head_dim * params.num_kv_heads * params.num_pages:
         raise ValueError("an MXFP4 pool is a uint8 tensor [num_pages, Hkv, 17 D]")
+    import torch
+    for t in rows:
+        if t.dtype != torch.bfloat16:
+            raise ValueError("q, K and V rows of an MXFP4 pool are bf16")
 
 
 def decode(q, pool, graph: HostGraph, params: Params, out=None, lse=None, stream=None):
@@ -241,7 +247,7 @@ def decode(q, pool, graph: HostGraph, params: Params, out=None, lse=None, stream
         out = torch.empty((B, params.num_q_heads, params.head_dim), dtype=odt, device=q.device)
     if lse is None:
         lse = torch.empty((B, params.num_q_heads), dtype=torch.float32, device=q.device)
-    _check_pool(pool, params)
+    _check_pool(pool, params, q)
     _check(lib.graphattn_decode(_dev_ptr(q), _dev_ptr(pool), ctypes.byref(graph.st),
                                 ctypes.byref(graph.bp), _dev_ptr(out), _dev_ptr(lse),
                                 ctypes.byref(params), _stream_handle(stream)))
@@ -252,7 +258,7 @@ def decode_static(q, pool, graph: HostGraph, params: Params, out, lse, stream=No
     """graphattn_decode_static: graphattn_decode with its workspace in the library's static
     device array (no allocation; the caller passes out and lse)."""
     lib = load_library()
-    _check_pool(pool, params)
+    _check_pool(pool, params, q)
     _check(lib.graphattn_decode_static(_dev_ptr(q), _dev_ptr(pool), ctypes.byref(graph.st),
                                        ctypes.byref(graph.bp), _dev_ptr(out), _dev_ptr(lse),
                                        ctypes.byref(params), _stream_handle(stream)))
@@ -278,7 +284,7 @@ def extend(q, pool, graph: HostGraph, query_counts, params: Params, out=None, ls
         out = torch.empty((R, params.num_q_heads, params.head_dim), dtype=odt, device=q.device)
     if lse is None:
         lse = torch.empty((R, params.num_q_heads), dtype=torch.float32, device=q.device)
-    _check_pool(pool, params)
+    _check_pool(pool, params, q)
     _check(lib.graphattn_extend(_dev_ptr(q), _dev_ptr(pool), ctypes.byref(graph.st),
                                 ctypes.byref(graph.bp), _ptr(cnt, ctypes.c_int32), _dev_ptr(out),
                                 _dev_ptr(lse), ctypes.byref(params), _stream_handle(stream)))
@@ -291,7 +297,7 @@ def kv_append(pool, k_new, v_new, slot_words, params: Params, stream=None):
     n = int(slot_words.numel())
     if k_new.shape[0] != n or v_new.shape[0] != n:
         raise ValueError("one K row and one V row per slot word")
-    _check_pool(pool, params)
+    _check_pool(pool, params, k_new, v_new)
     _check(lib.graphattn_kv_append(_dev_ptr(pool), _dev_ptr(k_new), _dev_ptr(v_new),
                                    _dev_ptr(slot_words), n, ctypes.byref(params),
                                    _stream_handle(stream)))
@@ -507,7 +513,7 @@ class Plan:
         _check(self.lib.graphattn_schedule(self.handle, _stream_handle(stream)))
 
     def run(self, q, pool, out, lse, stream=None):
-        _check_pool(pool, self.params)
+        _check_pool(pool, self.params, q)
         _check(self.lib.graphattn_run(self.handle, _dev_ptr(q), _dev_ptr(pool), _dev_ptr(out),
                                       _dev_ptr(lse), _stream_handle(stream)))
 
@@ -516,7 +522,7 @@ class Plan:
         (lse as run() wrote it), added to decay x mass_in (float32 [num_pages x 16])."""
         import torch
         p = self.params
-        _check_pool(pool, p)
+        _check_pool(pool, p, q)
         if q.numel() < self.rows * p.num_q_heads * p.head_dim or \
                 lse.numel() < self.rows * p.num_q_heads:
             raise ValueError("one row of q and of lse per query")

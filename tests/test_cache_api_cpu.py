@@ -178,9 +178,15 @@ def test_binding_refuses_tensors_of_other_types_and_sizes():
                      lambda: G.kv_read(bad, words, p, kv, kv)):
             with pytest.raises(ValueError, match="MXFP4 pool"):
                 call()
+    for k, v in ((kv.float(), kv), (kv, kv.to(torch.float8_e4m3fn))):
+        with pytest.raises(ValueError, match="bf16"):
+            G.kv_append(pool, k, v, words, p)
     with pytest.raises(ValueError, match="must be"):
         G.kv_read(pool, words, p, kv.half(), kv)
     with pytest.raises(ValueError, match="int32"):
         G.kv_read(pool, words.long(), p, kv, kv)
     with pytest.raises(ValueError, match="Hkv, D"):
         G.kv_read(pool, words, p, kv[:1], kv)
+    g = G.HostGraph([20], [0, 2], [0, 1], [0, 1], [0])
+    with pytest.raises(ValueError, match="bf16"):
+        G.decode_static(torch.zeros(1, 4, 64), pool, g, p, None, None)
