@@ -44,7 +44,8 @@ ga_status graphattn_kv_read(const void* kv_page_pool, const int32_t* slot_words,
  * first.  A row whose lse is infinite counts for nothing; a token with a score that is NaN, or +infinite in
  * such a row, has mass NaN.  Sums are float32, and the same bits for the
  * same inputs.  A plan without a current schedule is scheduled first.  GA_EINVAL where two segments on
- * paths own the same page (their slots would be written twice) and for a decay that is not finite.
+ * paths own the same page (their slots would be written twice) and for a decay that is not finite,
+ * GA_EUNSUPPORTED for a plan of 2^22 chains or with a chain of more than some four million tokens.
  * Decode and multi-query plans, all pool types; asynchronous on hip_stream, and calls on one plan do not
  * overlap with its other calls (graphattn_run). */
 ga_status graphattn_run_mass(ga_plan* plan, const void* q, const void* kv_page_pool,

@@ -118,7 +118,8 @@ struct ga_plan {
   bool updatable = false;
   std::vector<int64_t> h_page_off;
   std::vector<int32_t> h_pages;
-  int32_t mass_cost = 0, mass_parts = 0;    // how the attention mass takes the chains (0: not looked yet)
+  int32_t mass_cost = 0;       // how the attention mass takes the chains (0: not looked yet)
+  int32_t mass_parts = 0, mass_parts_huge = 0;
   bool mass_many = false;
   int distinct = -1;               // no page twice among the segments on a path (-1: not looked yet)
   std::vector<int32_t> h_last, h_counts;
@@ -892,6 +893,30 @@ ga_status plan_mass_args(ga_plan* plan, bool schedule, hipStream_t stream, MassA
     plan->distinct = twice ? 0 : 1;
   }
   if (!plan->distinct) return fail(GA_EINVAL, "two segments of the plan own the same page");
+  if (plan->z.S > kMassChains)
+    return fail(GA_EUNSUPPORTED, "%d chains (> %d)", plan->z.S, kMassChains);
+  if (!plan->mass_cost) {
+    // What a workgroup takes: as much as leaves every CU several workgroups.
+    const CGraph& c = plan->cg;
+    std::vector<int64_t> rows(plan->z.S, 0);
+    for (const int32_t v : c.path_segs) rows[v] += plan->p.num_q_heads / plan->p.num_kv_heads;
+    int32_t cost = ga::kMassCost;
+    for (;; cost /= 2) {
+      int64_t parts = 0;
+      for (int32_t v = 0; v < plan->z.S; ++v) parts += ga::mass_parts(c.npg[v], rows[v], cost);
+      if (cost <= 4 || parts >= 12LL * plan->num_cus) break;
+    }
+    // (all pages a chain owns: later lengths may use them)
+    for (int32_t v = 0; v < plan->z.S; ++v) {
+      int32_t& most = rows[v] > ga::kMassHuge ? plan->mass_parts_huge : plan->mass_parts;
+      most = std::max(most, ga::mass_parts(c.seg_page_off[v + 1] - c.seg_page_off[v], rows[v], cost));
+      plan->mass_many = plan->mass_many || (rows[v] > ga::kMassRows && rows[v] <= ga::kMassHuge);
+    }
+    plan->mass_cost = cost;
+  }
+  if (std::max(plan->mass_parts, plan->mass_parts_huge) > kMassParts)
+    return fail(GA_EUNSUPPORTED, "a chain is too long (%d parts)",
+                std::max(plan->mass_parts, plan->mass_parts_huge));
   if (schedule && !plan->scheduled) {
     const ga_status rc = do_schedule(plan, stream);
     if (rc) return rc;
@@ -909,28 +934,11 @@ ga_status plan_mass_args(ga_plan* plan, bool schedule, hipStream_t stream, MassA
   a->dtype = plan->p.dtype;
   a->causal = plan->causal;
   a->scale_log2 = plan->p.softmax_scale * 1.4426950408889634f;
-  if (!plan->mass_cost) {
-    // What a workgroup takes: as much as leaves every CU several workgroups.
-    const CGraph& c = plan->cg;
-    std::vector<int64_t> rows(plan->z.S, 0);
-    for (const int32_t v : c.path_segs) rows[v] += plan->p.num_q_heads / plan->p.num_kv_heads;
-    int32_t cost = ga::kMassCost;
-    for (;; cost /= 2) {
-      int64_t parts = 0;
-      for (int32_t v = 0; v < plan->z.S; ++v) parts += ga::mass_parts(c.npg[v], rows[v], cost);
-      if (cost <= 4 || parts >= 12LL * plan->num_cus) break;
-    }
-    // (all pages a chain owns: later lengths may use them)
-    for (int32_t v = 0; v < plan->z.S; ++v)
-      plan->mass_parts = std::max(plan->mass_parts,
-                                  ga::mass_parts(c.seg_page_off[v + 1] - c.seg_page_off[v], rows[v], cost));
-    for (const int64_t r : rows) plan->mass_many = plan->mass_many || r > ga::kMassRows;
-    plan->mass_cost = cost;
-  }
   a->chains = plan->z.S;
   a->cost = plan->mass_cost;
-  a->many = plan->mass_many;
   a->parts = plan->mass_parts;
+  a->parts_huge = plan->mass_parts_huge;
+  a->many = plan->mass_many;
   return GA_OK;
 }
 

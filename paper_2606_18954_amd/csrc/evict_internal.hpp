@@ -24,12 +24,15 @@ struct MassArgs {
   int32_t Hq, Hkv, group, head_dim, dtype;
   bool causal;             // a multi-query plan
   float scale_log2, decay;
-  int32_t chains, parts;   // chains, and the most parts one of them may have
+  int32_t chains;
+  int32_t parts, parts_huge;   // the most parts a chain of up to, of more than kMassHuge rows may have (0: none)
+  bool many;                   // some chain has more than kMassRows rows, and up to kMassHuge
   int32_t cost;            // what a workgroup takes: pages x pairs of row tiles
-  bool many;               // some chain has more than kMassRows rows
 };
 // Rows of a chain that are taken two tiles at a time.
 constexpr int32_t kMassRows = 128;
+// Rows from which on workgroups of sixteen waves share them.
+constexpr int32_t kMassHuge = 4096;
 constexpr int32_t kMassCost = 128;     // most of it, and so most pages
 // Parts a chain is taken in: of about `cost` pages x pairs of row tiles, and of kMassPages pages at least.
 constexpr int32_t kMassPages = 4;
@@ -40,6 +43,8 @@ __host__ __device__ inline int32_t mass_parts(int64_t pages, int64_t rows, int32
   const int32_t most = (int32_t)((pages + kMassPages - 1) / kMassPages);
   return parts < most ? parts : most;
 }
+// Limits of a launch's grid: its first extent counts threads in 32 bits, the second one ends here.
+constexpr int32_t kMassChains = (1 << 22) - 1, kMassParts = 65535;
 hipError_t launch_mass(const MassArgs& a, hipStream_t stream);
 
 // The schedule and sizes of a plan as the mass kernel needs them (api.cpp); rows: query rows.

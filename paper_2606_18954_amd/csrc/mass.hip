@@ -12,8 +12,12 @@
 //
 // Few rows (up to kMassRows, most chains of a decode step): two tiles' queries stay in registers and
 // the pages stream past, several of them on their way, once per two tiles (from the caches after the first
-// time).  More rows (prefill): a few pages stay, as matrix operands, and the rows stream past, one tile's
-// queries and the next one's row numbers on their way.
+// time).  More rows: a few pages stay, as matrix operands, and the rows stream past, one tile's queries and the
+// next one's row numbers on their way.  A great many (more than kMassHuge, a prompt's prefill): the same by
+// workgroups of sixteen waves, which share the rows of their four pages; a kernel of its own.  (24 prompts of up
+// to 1700 tokens, MXFP4, with four waves | sixteen: 28/4 heads x 128 555 | 425 us, 16/2 x 64 373 | 134; chains of
+// fewer rows lose by it, their workgroups' starts are no longer hidden by each other: merged graphs with 16
+// queries a branch, up to 1800 rows, 431 | 570.)
 //
 // What bounds it: reading K.  1024 branches of merged graphs, 28/4 heads x 128, MXFP4: 129 us, 0.65 GB read at
 // 5.0 TB/s (0.50 GB of them once; the rest are scales' half lines, queries and last pages read again), vector
@@ -35,10 +39,14 @@ namespace {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-// Waves per SIMD the registers are kept to.
-constexpr int mass_waves(int D, int type, bool many) {
-  return type == GA_F32 ? (D == 64 ? 4 : 2) : !many || D == 64 ? 4 : 3;
+// Waves of a workgroup, and waves per SIMD the registers are kept to.
+constexpr int mass_wg_waves(int kind) { return kind == 2 ? 16 : 4; }
+constexpr int mass_waves(int D, int type, int kind) {
+  return kind == 2 || D == 64 ? 4 : type == GA_F32 ? 2 : kind == 1 ? 3 : 4;
 }
+// Pages of a part of more than kMassHuge rows (mass_parts), at most.
+constexpr int kMassHugePages = 4;
+static_assert(kMassHuge / 32 >= kMassCost && kMassPages <= kMassHugePages);
 
 template <int D, int TYPE>
 struct MCfg {
@@ -56,7 +64,9 @@ template <bool F32> struct Op;
 template <> struct Op<true> { float v; };
 template <> struct Op<false> { bf16x8 v; };
 
-// One page's K as loaded: token r16, channels kg D / 4 ..+ D / 4 - 1.
+// One page's K as loaded: token r16.  The order of the channels in the contraction is free, as long as Q's is
+// the same: the 16-byte pieces 4 i + kg of a row, so that the four lanes of a row load 64 neighbouring bytes;
+// MXFP4: the channels kg D / 4 ..+ D / 4 - 1, whose codes are one load.
 template <int D, int TYPE>
 struct RawK {
   u32x4 w[(MCfg<D, TYPE>::NW + 3) / 4];
@@ -80,9 +90,8 @@ __device__ __forceinline__ void load_k(RawK<D, TYPE>& k, page_t page, int r16, i
     }
     k.scale = load4(page, Fp4<D>::KS + (scale_byte<D>(r16, kg) & ~3u));
   } else {
-    const unsigned off = (r16 * D + kg * (D / 4)) * C::ELT;
 #pragma unroll
-    for (int i = 0; i < C::NW / 4; ++i) k.w[i] = load16(page, off + 16 * i);
+    for (int i = 0; i < C::NW / 4; ++i) k.w[i] = load16(page, r16 * D * C::ELT + 64 * i + 16 * kg);
   }
 }
 template <int D, int TYPE, int S>
@@ -102,20 +111,21 @@ __device__ __forceinline__ Op<MCfg<D, TYPE>::F32> operand(const RawK<D, TYPE>& k
   return o;
 }
 // The lane's operands of one row of Q: the same channels.
-template <int D, bool F32>
+template <int D, int TYPE, bool F32 = TYPE == GA_F32>
 __device__ __forceinline__ void load_row(Op<F32> (&op)[F32 ? D / 4 : D / 32], const unsigned char* p,
                                          int kg) {
-  if constexpr (F32) {
+  if constexpr (TYPE == GA_F32) {
 #pragma unroll
     for (int s = 0; s < D / 16; ++s) {
-      const f32x4 x = *reinterpret_cast<const f32x4*>(p + kg * D + 16 * s);
+      const f32x4 x = *reinterpret_cast<const f32x4*>(p + 64 * s + 16 * kg);
 #pragma unroll
       for (int i = 0; i < 4; ++i) op[4 * s + i].v = x[i];
     }
   } else {
 #pragma unroll
     for (int s = 0; s < D / 32; ++s)
-      op[s].v = *reinterpret_cast<const bf16x8*>(p + kg * (D / 2) + 16 * s);
+      op[s].v = *reinterpret_cast<const bf16x8*>(
+          p + (TYPE == GA_MXFP4 ? kg * (D / 2) + 16 * s : 64 * s + 16 * kg));
   }
 }
 template <bool F32>
@@ -138,21 +148,23 @@ __device__ __forceinline__ float offset_of(float lse, bool live) {
                                                      : -__builtin_huge_valf();
 }
 
-// MANY: some chain has more than kMassRows rows.  (The other variant has a third fewer registers, and so
-// more waves to hide the loads of a workgroup's start.)
-template <int D, int TYPE, bool CAUSAL, bool MANY>
-__global__ __launch_bounds__(256, mass_waves(D, TYPE, MANY)) void k_mass(MassArgs a) {
+// KIND 0: no chain has more than kMassRows rows, 1: some have, up to kMassHuge, 2: the chains of more.  (Kind 0
+// has a third fewer registers than 1, and so more waves to hide the loads of a workgroup's start.)
+template <int D, int TYPE, bool CAUSAL, int KIND>
+__global__ __launch_bounds__(64 * mass_wg_waves(KIND), mass_waves(D, TYPE, KIND)) void k_mass(MassArgs a) {
+  constexpr int NWV = mass_wg_waves(KIND);
+  constexpr bool HUGE_ROWS = KIND == 2;
   using C = MCfg<D, TYPE>;
   using OpT = Op<C::F32>;
-  extern __shared__ float s_mass[];                 // [kv-head slot][page][token]
+  extern __shared__ float s_mass[];                 // [kv-head slot (x split)][page][token]
   // (part by part: those that most chains do not have come last)
-  const int part = (int)blockIdx.x / a.chains;
-  const int v = (int)blockIdx.x - part * a.chains;
+  const int part = (int)blockIdx.y, v = (int)blockIdx.x;
   const int np_all = (a.seg_len[v] + kPageTokens - 1) / kPageTokens;
   const int64_t page0 = a.seg_page_off[v], goff = a.grp_off[v];
   const int cnt = (int)(a.grp_off[v + 1] - goff);
   const int cw = CAUSAL ? a.seg_causal[v] : kNoCausal;
   const int rows = cnt * a.group;
+  if (HUGE_ROWS != rows > kMassHuge) return;              // (the other kernel's)
   const int nparts = mass_parts(np_all, rows, a.cost);    // equal ones
   if (part >= nparts) return;
   const int per = (np_all + nparts - 1) / nparts;
@@ -166,7 +178,7 @@ __global__ __launch_bounds__(256, mass_waves(D, TYPE, MANY)) void k_mass(MassArg
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r16 = lane & 15, kg = lane >> 4;
   const int hs = a.Hkv >= 4 ? 4 : a.Hkv >= 2 ? 2 : 1;     // waves that take different kv-heads
-  const int rs = 4 / hs;                                  // waves that share a head's pages
+  const int rs = NWV / hs;                                // waves that share a head: its pages, or its rows
   const int hslot = wave % hs, split = wave / hs;
   const unsigned char* q = static_cast<const unsigned char*>(a.q);
   const int pw0 = words[min(lane, npg - 1)], pw1 = words[min(64 + lane, npg - 1)];   // a lane per page
@@ -179,7 +191,14 @@ __global__ __launch_bounds__(256, mass_waves(D, TYPE, MANY)) void k_mass(MassArg
     gi = r - j * a.group;
     if (gi >= a.group) { gi -= a.group; ++j; }
   };
-  float* region = s_mass + hslot * a.cost * kPageTokens;
+  const int stride = (HUGE_ROWS ? kMassHugePages : a.cost) * kPageTokens;
+  // The waves of a head take different pages; of a chain with a great many rows, a part of which has few, those
+  // left take different rows.
+  int psplit = rs;
+  if constexpr (HUGE_ROWS)
+    while (psplit > 1 && (psplit / 2) * C::PG >= npg) psplit /= 2;
+  const int rsplit = rs / psplit;
+  float* region = s_mass + (hslot + split / psplit * hs) * stride;
   // The first tile with a row that sees the page (a newest segment: its last row sees every page).
   auto first_tile = [&](int page) {
     return cm ? (int)(((int64_t)max(0, kPageTokens * page - cw) * a.group) >> 4) : 0;
@@ -211,7 +230,7 @@ __global__ __launch_bounds__(256, mass_waves(D, TYPE, MANY)) void k_mass(MassArg
     };
     // (A slot past the segment's end may hold anything: only its own sums see it, and they are not
     // stored.)
-    auto few = [&](auto nt_tag, int t0) {
+    auto few = [&](auto nt_tag, int t0, bool fresh) {
       constexpr int NT = decltype(nt_tag)::value;
       OpT qo[NT][C::OPS];
       float lse[NT], nl[NT][4];
@@ -221,7 +240,7 @@ __global__ __launch_bounds__(256, mass_waves(D, TYPE, MANY)) void k_mass(MassArg
         int j, gi;
         split_row(min(16 * (t0 + t) + r16, rows - 1), j, gi);
         const int64_t row = (int64_t)branches[j] * a.Hq + h * a.group + gi;
-        load_row<D, C::F32>(qo[t], q + row * D * C::ELT, kg);
+        load_row<D, TYPE>(qo[t], q + row * D * C::ELT, kg);
         lse[t] = a.lse[row];
         rank[t] = j;
       }
@@ -269,14 +288,14 @@ __global__ __launch_bounds__(256, mass_waves(D, TYPE, MANY)) void k_mass(MassArg
               }
               x += (e[0] + e[1]) + (e[2] + e[3]);
             }
-            put(p, x, h == hslot && t0 == tile0);
+            put(p, x, fresh);
           }
           load_k<D, TYPE>(buf[i], page_of(p + rs * C::PF), r16, kg);
         }
       }
     };
     auto many = [&] {
-      for (int p0 = C::PG * split; p0 < npg; p0 += C::PG * rs) {
+      for (int p0 = C::PG * (split % psplit); p0 < npg; p0 += C::PG * psplit) {
         OpT kb[C::PG][C::OPS];
         {
           RawK<D, TYPE> raw[C::PG];
@@ -292,24 +311,28 @@ __global__ __launch_bounds__(256, mass_waves(D, TYPE, MANY)) void k_mass(MassArg
         float acc[C::PG];
 #pragma unroll
         for (int g = 0; g < C::PG; ++g) acc[g] = 0.f;
-        int t = first_tile(pg0 + p0);
         // Row of the lane in tile x: its number in q (clamped to the last row), and its rank.
         auto row_of = [&](int x, int& j) {
           int gi;
           split_row(min(16 * x + r16, rows - 1), j, gi);
           return (int64_t)branches[j] * a.Hq + h * a.group + gi;
         };
+        // The next tile's queries, and the row numbers of the one behind it, are on their way (sixteen waves have
+        // registers for the row numbers only).
+        int t = first_tile(pg0 + p0) + split / psplit, j0 = 0, j1 = 0;
         OpT qo[C::OPS], qn[C::OPS];
-        int j0 = 0, j1 = 0;
-        int64_t row1 = row_of(t, j0);
-        float l0 = a.lse[row1], l1 = 0.f;
-        load_row<D, C::F32>(qo, q + row1 * D * C::ELT, kg);
-        row1 = row_of(t + 1, j1);
-        for (; t < ntile; ++t) {
-          load_row<D, C::F32>(qn, q + row1 * D * C::ELT, kg);
-          l1 = a.lse[row1];
+        int64_t row = row_of(t, j0);
+        float l0 = 0.f, l1 = 0.f;
+        if constexpr (!HUGE_ROWS) {
+          l0 = a.lse[row];
+          load_row<D, TYPE>(qo, q + row * D * C::ELT, kg);
+          row = row_of(t + rsplit, j1);
+        }
+        for (; t < ntile; t += rsplit) {
+          load_row<D, TYPE>(HUGE_ROWS ? qo : qn, q + row * D * C::ELT, kg);
+          (HUGE_ROWS ? l0 : l1) = a.lse[row];
           int j2;
-          row1 = row_of(t + 2, j2);
+          row = row_of(t + (HUGE_ROWS ? 1 : 2) * rsplit, j2);
           f32x4 S[C::PG];
 #pragma unroll
           for (int g = 0; g < C::PG; ++g) S[g] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -338,35 +361,39 @@ __global__ __launch_bounds__(256, mass_waves(D, TYPE, MANY)) void k_mass(MassArg
             for (int i = 0; i < 4; ++i) e[i] = exp2_(fmaf(S[g][i], a.scale_log2, nl[i]));
             acc[g] += (e[0] + e[1]) + (e[2] + e[3]);
           }
+          if constexpr (HUGE_ROWS) {
+            j0 = j2;
+          } else {
 #pragma unroll
-          for (int s = 0; s < C::OPS; ++s) qo[s] = qn[s];
-          l0 = l1;
-          j0 = j1;
-          j1 = j2;
+            for (int s = 0; s < C::OPS; ++s) qo[s] = qn[s];
+            l0 = l1;
+            j0 = j1;
+            j1 = j2;
+          }
         }
 #pragma unroll
         for (int g = 0; g < C::PG; ++g)
           if (p0 + g < npg) put(p0 + g, acc[g], h == hslot);
       }
     };
-    if (MANY && rows > kMassRows) {
-      if constexpr (MANY) many();
-    } else {
+    if (HUGE_ROWS || (KIND == 1 && rows > kMassRows)) {
+      if constexpr (KIND > 0) many();
+    } else if constexpr (!HUGE_ROWS) {
       int t = tile0;
-      for (; t + 1 < ntile; t += 2) few(std::integral_constant<int, 2>{}, t);
-      if (t < ntile) few(std::integral_constant<int, 1>{}, t);
+      for (; t + 1 < ntile; t += 2) few(std::integral_constant<int, 2>{}, t, h == hslot && t == tile0);
+      if (t < ntile) few(std::integral_constant<int, 1>{}, t, h == hslot && t == tile0);
     }
   }
   // The slots' earlier mass is on its way while the last waves come in.
-  constexpr int IN = kMassCost / 16;
+  constexpr int PPI = 4 * NWV, IN = kMassCost / PPI;   // pages at a time
   float in[IN];
   int64_t slot[IN];
 #pragma unroll
   for (int i = 0; i < IN; ++i) {
-    const int p = i * 16 + (tid >> 4), tok = tid & 15;
+    const int p = i * PPI + (tid >> 4), tok = tid & 15;
     slot[i] = -1;
     in[i] = 0.f;
-    if (i * 16 < npg && p < npg) {
+    if (i * PPI < npg && p < npg) {
       const int word = words[p];
       if (tok <= (int)((unsigned)word >> kPageValidShift)) {
         slot[i] = (int64_t)(word & kPageIdMask) * kPageTokens + tok;
@@ -378,43 +405,42 @@ __global__ __launch_bounds__(256, mass_waves(D, TYPE, MANY)) void k_mass(MassArg
 #pragma unroll
   for (int i = 0; i < IN; ++i) {
     if (slot[i] < 0) continue;
-    const int p = i * 16 + (tid >> 4), tok = tid & 15;
+    const int p = i * PPI + (tid >> 4), tok = tid & 15;
     float sum = 0.f;
-    for (int k = 0; k < hs; ++k) {
-      sum += s_mass[(k * a.cost + p) * kPageTokens + tok];
-    }
+    for (int k = 0; k < hs * rsplit; ++k) sum += s_mass[k * stride + p * kPageTokens + tok];
     a.mass_out[slot[i]] = a.mass_in ? fmaf(a.decay, in[i], sum) : sum;
   }
 }
 
 template <int D>
 hipError_t launch_t(const MassArgs& a, hipStream_t stream) {
-  const int64_t grid = (int64_t)a.chains * a.parts;
-  if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
-  const unsigned lds = 4 * a.cost * kPageTokens * sizeof(float);
-  auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), lds, stream, a);
-  };
-  auto type = [&](auto causal) {
+  auto type = [&](auto causal, auto kind) {
     constexpr bool CAUSAL = decltype(causal)::value;
-    auto rows = [&](auto many) {
-      constexpr bool MANY = decltype(many)::value;
-      if (a.dtype == GA_F32) go(k_mass<D, GA_F32, CAUSAL, MANY>);
-      else if (a.dtype == GA_BF16) go(k_mass<D, GA_BF16, CAUSAL, MANY>);
-      else go(k_mass<D, GA_MXFP4, CAUSAL, MANY>);
+    constexpr int KIND = decltype(kind)::value, NWV = mass_wg_waves(KIND);
+    const int parts = KIND == 2 ? a.parts_huge : a.parts;
+    if (parts == 0) return;
+    const unsigned lds = (KIND == 2 ? NWV * kMassHugePages : 4 * a.cost) * kPageTokens * sizeof(float);
+    auto go = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, dim3((unsigned)a.chains, (unsigned)parts), dim3(64 * NWV), lds, stream, a);
     };
-    if (a.many) rows(std::true_type{});
-    else rows(std::false_type{});
+    if (a.dtype == GA_F32) go(k_mass<D, GA_F32, CAUSAL, KIND>);
+    else if (a.dtype == GA_BF16) go(k_mass<D, GA_BF16, CAUSAL, KIND>);
+    else go(k_mass<D, GA_MXFP4, CAUSAL, KIND>);
   };
-  if (a.causal) type(std::true_type{});
-  else type(std::false_type{});
+  auto kinds = [&](auto causal) {
+    type(causal, std::integral_constant<int, 2>{});
+    if (a.many) type(causal, std::integral_constant<int, 1>{});
+    else type(causal, std::integral_constant<int, 0>{});
+  };
+  if (a.causal) kinds(std::true_type{});
+  else kinds(std::false_type{});
   return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_mass(const MassArgs& a, hipStream_t stream) {
-  if (a.chains == 0 || a.parts == 0) return hipSuccess;
+  if (a.chains == 0) return hipSuccess;
   if (a.head_dim == 64) return launch_t<64>(a, stream);
   if (a.head_dim == 128) return launch_t<128>(a, stream);
   return hipErrorInvalidValue;

@@ -101,6 +101,22 @@ def test_mass_of_many_rows():
     _check_mass(rng, g, 14, 2, 64, "bf16")
 
 
+@pytest.mark.parametrize("Hq,Hkv,D,dtype", [(16, 2, 64, "mxfp4"), (7, 1, 128, "bf16"), (24, 3, 64, "f32"),
+                                             (28, 4, 128, "mxfp4"), (8, 1, 128, "f32")])
+def test_mass_of_a_great_many_rows(Hq, Hkv, D, dtype):
+    """One plan with a chain of more than 4096 rows a kv-head (a prompt's prefill: workgroups of sixteen waves),
+    one of a few hundred (a shared prefix of several branches) and one of few."""
+    require_gpu()
+    say(f"[case] mass of a great many rows {Hq}/{Hkv}/{D} {dtype}")
+    rng = np.random.default_rng(Hq)
+    n = 4100 * Hkv // Hq + 7
+    lens, paths = [n, 75, 40, 40, 90], [[0], [1, 2], [1, 3], [4]]
+    counts = [n, 40, 33, 2]
+    g = W.assemble_graph(lens, paths, 6, slack_pages=2)
+    assert n * Hq // Hkv > 4096 and 73 * Hq // Hkv > 128 and 2 * Hq // Hkv < 128
+    _check_mass(rng, g, Hq, Hkv, D, dtype, counts)
+
+
 def test_rows_without_weight_count_for_nothing_and_no_mass_in():
     require_gpu()
     say("[case] infinite lse")
