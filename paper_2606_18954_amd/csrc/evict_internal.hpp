@@ -31,7 +31,7 @@ struct MassArgs {
 };
 // Rows of a chain that are taken two tiles at a time.
 constexpr int32_t kMassRows = 128;
-// Rows from which on workgroups of sixteen waves share them.
+// Rows from which on workgroups of more waves share them.
 constexpr int32_t kMassHuge = 4096;
 constexpr int32_t kMassCost = 128;     // most of it, and so most pages
 // Parts a chain is taken in: of about `cost` pages x pairs of row tiles, and of kMassPages pages at least.

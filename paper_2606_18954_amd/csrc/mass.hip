@@ -14,10 +14,14 @@
 // the pages stream past, several of them on their way, once per two tiles (from the caches after the first
 // time).  More rows: a few pages stay, as matrix operands, and the rows stream past, one tile's queries and the
 // next one's row numbers on their way.  A great many (more than kMassHuge, a prompt's prefill): the same by
-// workgroups of sixteen waves, which share the rows of their four pages; a kernel of its own.  (24 prompts of up
-// to 1700 tokens, MXFP4, with four waves | sixteen: 28/4 heads x 128 555 | 425 us, 16/2 x 64 373 | 134; chains of
-// fewer rows lose by it, their workgroups' starts are no longer hidden by each other: merged graphs with 16
-// queries a branch, up to 1800 rows, 431 | 570.)
+// workgroups of twelve (head_dim 64: sixteen) waves, which share the rows of their four pages; a kernel of its own.
+// (24 prompts of up to 1700 tokens, MXFP4, with four waves | so: 28/4 heads x 128 555 | 404 us, 16/2 x 64 373 | 124;
+// chains of fewer rows lose by it, their workgroups' starts are no longer hidden by each other: merged graphs
+// with 16 queries a branch, up to 1800 rows, 431 | 570.  A wave's step, a tile of rows against four pages, then
+// takes a memory latency, 2200 cycles at three waves per SIMD, where its instructions take 730 for all three.
+// Without gain: rows from the last one down, which reads the queries from memory once and not three times; the
+// mask only where it is needed; sixteen waves of fewer registers, which leave no next tile's queries on their way,
+// 425.)
 //
 // What bounds it: reading K.  1024 branches of merged graphs, 28/4 heads x 128, MXFP4: 129 us, 0.65 GB read at
 // 5.0 TB/s (0.50 GB of them once; the rest are scales' half lines, queries and last pages read again), vector
@@ -40,9 +44,9 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 // Waves of a workgroup, and waves per SIMD the registers are kept to.
-constexpr int mass_wg_waves(int kind) { return kind == 2 ? 16 : 4; }
+constexpr int mass_wg_waves(int D, int kind) { return kind < 2 ? 4 : D == 64 ? 16 : 12; }
 constexpr int mass_waves(int D, int type, int kind) {
-  return kind == 2 || D == 64 ? 4 : type == GA_F32 ? 2 : kind == 1 ? 3 : 4;
+  return D == 64 ? 4 : kind == 2 ? 3 : type == GA_F32 ? 2 : kind == 1 ? 3 : 4;
 }
 // Pages of a part of more than kMassHuge rows (mass_parts), at most.
 constexpr int kMassHugePages = 4;
@@ -151,8 +155,8 @@ __device__ __forceinline__ float offset_of(float lse, bool live) {
 // KIND 0: no chain has more than kMassRows rows, 1: some have, up to kMassHuge, 2: the chains of more.  (Kind 0
 // has a third fewer registers than 1, and so more waves to hide the loads of a workgroup's start.)
 template <int D, int TYPE, bool CAUSAL, int KIND>
-__global__ __launch_bounds__(64 * mass_wg_waves(KIND), mass_waves(D, TYPE, KIND)) void k_mass(MassArgs a) {
-  constexpr int NWV = mass_wg_waves(KIND);
+__global__ __launch_bounds__(64 * mass_wg_waves(D, KIND), mass_waves(D, TYPE, KIND)) void k_mass(MassArgs a) {
+  constexpr int NWV = mass_wg_waves(D, KIND);
   constexpr bool HUGE_ROWS = KIND == 2;
   using C = MCfg<D, TYPE>;
   using OpT = Op<C::F32>;
@@ -317,22 +321,17 @@ __global__ __launch_bounds__(64 * mass_wg_waves(KIND), mass_waves(D, TYPE, KIND)
           split_row(min(16 * x + r16, rows - 1), j, gi);
           return (int64_t)branches[j] * a.Hq + h * a.group + gi;
         };
-        // The next tile's queries, and the row numbers of the one behind it, are on their way (sixteen waves have
-        // registers for the row numbers only).
-        int t = first_tile(pg0 + p0) + split / psplit, j0 = 0, j1 = 0;
+        // The next tile's queries, and the row numbers of the one behind it, are on their way.
+        int t = first_tile(pg0 + p0) + split / psplit, j0, j1, j2;
         OpT qo[C::OPS], qn[C::OPS];
         int64_t row = row_of(t, j0);
-        float l0 = 0.f, l1 = 0.f;
-        if constexpr (!HUGE_ROWS) {
-          l0 = a.lse[row];
-          load_row<D, TYPE>(qo, q + row * D * C::ELT, kg);
-          row = row_of(t + rsplit, j1);
-        }
+        float l0 = a.lse[row], l1;
+        load_row<D, TYPE>(qo, q + row * D * C::ELT, kg);
+        row = row_of(t + rsplit, j1);
         for (; t < ntile; t += rsplit) {
-          load_row<D, TYPE>(HUGE_ROWS ? qo : qn, q + row * D * C::ELT, kg);
-          (HUGE_ROWS ? l0 : l1) = a.lse[row];
-          int j2;
-          row = row_of(t + (HUGE_ROWS ? 1 : 2) * rsplit, j2);
+          load_row<D, TYPE>(qn, q + row * D * C::ELT, kg);
+          l1 = a.lse[row];
+          row = row_of(t + 2 * rsplit, j2);
           f32x4 S[C::PG];
 #pragma unroll
           for (int g = 0; g < C::PG; ++g) S[g] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -361,15 +360,11 @@ __global__ __launch_bounds__(64 * mass_wg_waves(KIND), mass_waves(D, TYPE, KIND)
             for (int i = 0; i < 4; ++i) e[i] = exp2_(fmaf(S[g][i], a.scale_log2, nl[i]));
             acc[g] += (e[0] + e[1]) + (e[2] + e[3]);
           }
-          if constexpr (HUGE_ROWS) {
-            j0 = j2;
-          } else {
 #pragma unroll
-            for (int s = 0; s < C::OPS; ++s) qo[s] = qn[s];
-            l0 = l1;
-            j0 = j1;
-            j1 = j2;
-          }
+          for (int s = 0; s < C::OPS; ++s) qo[s] = qn[s];
+          l0 = l1;
+          j0 = j1;
+          j1 = j2;
         }
 #pragma unroll
         for (int g = 0; g < C::PG; ++g)
@@ -416,7 +411,7 @@ template <int D>
 hipError_t launch_t(const MassArgs& a, hipStream_t stream) {
   auto type = [&](auto causal, auto kind) {
     constexpr bool CAUSAL = decltype(causal)::value;
-    constexpr int KIND = decltype(kind)::value, NWV = mass_wg_waves(KIND);
+    constexpr int KIND = decltype(kind)::value, NWV = mass_wg_waves(D, KIND);
     const int parts = KIND == 2 ? a.parts_huge : a.parts;
     if (parts == 0) return;
     const unsigned lds = (KIND == 2 ? NWV * kMassHugePages : 4 * a.cost) * kPageTokens * sizeof(float);
