@@ -17,10 +17,13 @@
 // kEvictGroup: one workgroup of 1024 threads, a barrier a step.  Longer ones: the same, but the keys are
 // read again for every step.
 //
-// What bounds it: latency.  3266 segments of 64 to 1024 tokens (1.8 M tokens, 14 MB), half of them kept: 11 to 14
-// us, half of it the three dependent loads (segment, page word, mass) of each wave; 256 segments of 8192: 14 to
-// 15 us, one workgroup per CU with a barrier a step.  The bytes would take 2.8 and 2.4 us.  Bit by bit, and one token's loads after another's, they
-// took 15.4 and 20.2.
+// What bounds it: latency.  3266 segments of 64 to 1024 tokens (1.8 M tokens, 14 MB), half of them kept: 11 to
+// 14 us, half of it the three dependent loads (segment, page word, mass) of each wave; 256 segments of 8192:
+// 14 to 15 us, one workgroup per CU with a barrier a step.  The bytes would take 2.8 and 2.4 us.  Bit by bit,
+// and one token's loads after another's, they took 15.4 and 20.2.
+//
+// A segment that is read again must find the masses it found before; where another stream writes them
+// meanwhile, the choice is any, but nothing outside the segment's outputs is written and every search ends.
 #include "evict_internal.hpp"
 
 namespace ga {
@@ -58,8 +61,8 @@ __device__ __forceinline__ void tokens(const EvictArgs& a, const EvictSeg& s, in
   }
 }
 
-__device__ __forceinline__ int below(uint64_t m, int lane) {
-  (void)lane;
+// Lanes below this one in m.
+__device__ __forceinline__ int below(uint64_t m) {
   return (int)__builtin_amdgcn_mbcnt_hi((unsigned)(m >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)m, 0));
 }
 
@@ -105,7 +108,7 @@ struct Bounds {
 // Among the m = clo - chi <= 64 keys between the bounds, one a lane (0: none), the one at which need is reached
 // becomes the lower bound, with its neighbour above.
 __device__ __forceinline__ void rank_rest(Bounds& x, unsigned mine, int need) {
-  const int m = x.clo - x.chi, want = need - x.chi;
+  const int m = min(x.clo - x.chi, 64), want = need - x.chi;
   int above = 0, reach = 0;
   for (int j = 0; j < m; ++j) {
     const unsigned k = __builtin_amdgcn_readlane(mine, j);
@@ -113,7 +116,7 @@ __device__ __forceinline__ void rank_rest(Bounds& x, unsigned mine, int need) {
     reach += k >= mine;
   }
   const uint64_t at = __ballot(mine != 0 && above < want && want <= reach);
-  const int l = __builtin_ctzll(at);
+  const int l = at ? __builtin_ctzll(at) : 0;
   x.lo = __builtin_amdgcn_readlane(mine, l);
   x.hi = x.lo + 1;
   x.clo = x.chi + __builtin_amdgcn_readlane(reach, l);
@@ -207,7 +210,7 @@ __global__ __launch_bounds__(256) void k_evict_wave(EvictArgs a) {
 #pragma unroll
         for (int i = b; i < b + NB; ++i) {
           const uint64_t in = __ballot(x.holds(key[i]));
-          if (x.holds(key[i])) s_rest[wave][at + below(in, lane)] = key[i];
+          if (x.holds(key[i])) s_rest[wave][at + below(in)] = key[i];
           at += __builtin_popcountll(in);
         }
       });
@@ -227,12 +230,12 @@ __global__ __launch_bounds__(256) void k_evict_wave(EvictArgs a) {
       if (ties > 0) {                                // (the same in every lane)
         const bool eq = key[i] == T;
         const uint64_t me = __ballot(eq);
-        stay = stay || (eq && below(me, lane) < ties);
+        stay = stay || (eq && below(me) < ties);
         ties -= min(ties, (int)__builtin_popcountll(me));
       }
       const uint64_t ms = __ballot(stay);
       if (stay) {
-        const unsigned o = out + (unsigned)below(ms, lane);
+        const unsigned o = out + (unsigned)below(ms);
         if (positions) positions[o] = 64 * i + lane;
         if (words) words[o] = word[i];
       }
@@ -336,7 +339,7 @@ __global__ __launch_bounds__(1024) void k_evict_group(EvictArgs a) {
 #pragma unroll
           for (int i = b; i < b + NB; ++i) {
             const uint64_t in = __ballot(x.holds(key[i]));
-            if (x.holds(key[i])) s_rest[at + below(in, lane)] = key[i];
+            if (x.holds(key[i]) && (!LONG || at + below(in) < 64)) s_rest[at + below(in)] = key[i];
             at += __builtin_popcountll(in);
           }
         });
@@ -359,7 +362,7 @@ __global__ __launch_bounds__(1024) void k_evict_group(EvictArgs a) {
     T = x.clo == need ? x.lo - 1 : x.lo;
     ties = x.clo == need ? 0 : need - x.chi;
   }
-  int64_t out = s.out;
+  unsigned base = 0;                                 // tokens that stayed in the blocks before
   for (int blk = 0; blk < nblk; ++blk) {
     if (LONG) load(blk);
     // Per run of 64 tokens: keys above T and equal to it; then the running sums of both.
@@ -411,8 +414,8 @@ __global__ __launch_bounds__(1024) void k_evict_group(EvictArgs a) {
       }
     }
     __syncthreads();
-    int32_t* positions = a.positions ? a.positions + out : nullptr;
-    int32_t* words = a.words ? a.words + out : nullptr;
+    int32_t* positions = a.positions ? a.positions + s.out + base : nullptr;
+    int32_t* words = a.words ? a.words + s.out + base : nullptr;
     runs(blk, [&](int b) {
 #pragma unroll
       for (int i = b; i < b + NB; ++i) {
@@ -421,19 +424,19 @@ __global__ __launch_bounds__(1024) void k_evict_group(EvictArgs a) {
         if (ties > 0) {
           const int pe = s_eq[16 * i + wave];
           const bool eq = key[i] == T;
-          stay = stay || (eq && pe + below(__ballot(eq), lane) < ties);
+          stay = stay || (eq && pe + below(__ballot(eq)) < ties);
           o += (unsigned)min(pe, ties);
         }
         const uint64_t ms = __ballot(stay);
-        if (stay) {
-          o += (unsigned)below(ms, lane);
+        o += (unsigned)below(ms);
+        if (stay && (!LONG || base + o < (unsigned)s.keep)) {
           if (positions) positions[o] = blk * kEvictGroup + 1024 * i + tid;
           if (words) words[o] = word[i];
         }
       }
     });
     const int tg = s_sum[0], te = min(s_sum[1], ties);
-    out += tg + te;
+    base += (unsigned)(tg + te);
     ties -= te;
     __syncthreads();
   }
