@@ -1,6 +1,6 @@
-// Segment attention over MXFP4 pools (decode, and multi-query steps with few rows a page): one work item = (segment chain, page
-// chunk, row block of up to 128 query rows, kv-head), as in seg_attn.hip, with the work list, the
-// descriptors, the partial rows and the merge shared with it.
+// Segment attention over MXFP4 pools (decode, and multi-query steps with few rows a page): one work item =
+// (segment chain, page chunk, row block of up to 128 query rows, kv-head), as in seg_attn.hip, with the work
+// list, the descriptors, the partial rows and the merge shared with it.
 //
 //   S^T = K Q^T   (16 tokens x 16 rows per matrix tile, contraction over head_dim)
 //   O^T += V^T P^T (contraction over the 32 tokens of a pair of pages)

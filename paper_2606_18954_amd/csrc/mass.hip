@@ -153,7 +153,8 @@ __device__ __forceinline__ float offset_of(float lse, bool live) {
 }
 
 // KIND 0: no chain has more than kMassRows rows, 1: some have, up to kMassHuge, 2: the chains of more.  (Kind 0
-// has a third fewer registers than 1, and so more waves to hide the loads of a workgroup's start.)
+// has a third fewer registers than 1, and so more waves to hide the loads of a workgroup's start: merged graphs
+// of 1024 branches 135 us with kind 0, 145 with kind 1.)
 template <int D, int TYPE, bool CAUSAL, int KIND>
 __global__ __launch_bounds__(64 * mass_wg_waves(D, KIND), mass_waves(D, TYPE, KIND)) void k_mass(MassArgs a) {
   constexpr int NWV = mass_wg_waves(D, KIND);
