@@ -191,26 +191,31 @@ def make_params(num_q_heads: int, num_kv_heads: int, head_dim: int, num_pages: i
                   DTYPES.get(dtype, GA_F32), softmax_scale, int(bool(out_f32)))
 
 
-def _stream_getter():
-    """The function that gives the current stream's handle.  torch's raw getter, where it has one: a Stream
-    object costs 2.7 us, a third of a call that launches one small kernel; the getter 0.2 us."""
+_torch = None
+_raw_stream = None
+
+
+def _load_torch():
+    """torch, and its raw getter of a device's current stream, where it has one: a Stream object costs 2.7 us, a
+    third of a call that launches one small kernel; the getter 0.1 us."""
+    global _torch, _raw_stream
     import torch
-    device, raw = torch.cuda.current_device, getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    if raw is None:
-        return lambda: int(torch.cuda.current_stream().cuda_stream)
-    return lambda: int(raw(device()))
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    _torch = torch
+    return torch
 
 
-_current_stream = None
-
-
-def _stream_handle(stream) -> int:
-    global _current_stream
+def _stream_handle(stream, t=None) -> int:
+    """The stream's handle.  Without a stream a call goes to the current device's, where tensor t must live."""
     if stream is not None:
         return int(stream.cuda_stream)
-    if _current_stream is None:
-        _current_stream = _stream_getter()
-    return _current_stream()
+    torch = _torch or _load_torch()
+    device = torch.cuda.current_device()
+    if t is not None and t.get_device() != device:
+        raise ValueError(f"tensors live on device {t.get_device()}, the current one is {device}")
+    if _raw_stream is None:
+        return int(torch.cuda.current_stream().cuda_stream)
+    return int(_raw_stream(device))
 
 
 def _dev_ptr(t) -> int:
@@ -228,10 +233,10 @@ def _check_pool(pool, params: Params, *rows):
     layout would be read past their end."""
     if params.dtype != GA_MXFP4:
         return
-    if pool.element_size() != 1 or \
+    torch = _torch or _load_torch()
+    if pool.dtype != torch.uint8 or \
             pool.numel() < 17 * params.head_dim * params.num_kv_heads * params.num_pages:
         raise ValueError("an MXFP4 pool is a uint8 tensor [num_pages, Hkv, 17 D]")
-    import torch
     for t in rows:
         if t.dtype != torch.bfloat16:
             raise ValueError("q, K and V rows of an MXFP4 pool are bf16")
@@ -250,7 +255,7 @@ def decode(q, pool, graph: HostGraph, params: Params, out=None, lse=None, stream
     _check_pool(pool, params, q)
     _check(lib.graphattn_decode(_dev_ptr(q), _dev_ptr(pool), ctypes.byref(graph.st),
                                 ctypes.byref(graph.bp), _dev_ptr(out), _dev_ptr(lse),
-                                ctypes.byref(params), _stream_handle(stream)))
+                                ctypes.byref(params), _stream_handle(stream, pool)))
     return out, lse
 
 
@@ -261,7 +266,7 @@ def decode_static(q, pool, graph: HostGraph, params: Params, out, lse, stream=No
     _check_pool(pool, params, q)
     _check(lib.graphattn_decode_static(_dev_ptr(q), _dev_ptr(pool), ctypes.byref(graph.st),
                                        ctypes.byref(graph.bp), _dev_ptr(out), _dev_ptr(lse),
-                                       ctypes.byref(params), _stream_handle(stream)))
+                                       ctypes.byref(params), _stream_handle(stream, pool)))
     return out, lse
 
 
@@ -287,7 +292,7 @@ def extend(q, pool, graph: HostGraph, query_counts, params: Params, out=None, ls
     _check_pool(pool, params, q)
     _check(lib.graphattn_extend(_dev_ptr(q), _dev_ptr(pool), ctypes.byref(graph.st),
                                 ctypes.byref(graph.bp), _ptr(cnt, ctypes.c_int32), _dev_ptr(out),
-                                _dev_ptr(lse), ctypes.byref(params), _stream_handle(stream)))
+                                _dev_ptr(lse), ctypes.byref(params), _stream_handle(stream, pool)))
     return out, lse
 
 
@@ -300,7 +305,7 @@ def kv_append(pool, k_new, v_new, slot_words, params: Params, stream=None):
     _check_pool(pool, params, k_new, v_new)
     _check(lib.graphattn_kv_append(_dev_ptr(pool), _dev_ptr(k_new), _dev_ptr(v_new),
                                    _dev_ptr(slot_words), n, ctypes.byref(params),
-                                   _stream_handle(stream)))
+                                   _stream_handle(stream, pool)))
 
 
 def kv_copy(pool, src_words, dst_words, params: Params, stream=None):
@@ -311,13 +316,13 @@ def kv_copy(pool, src_words, dst_words, params: Params, stream=None):
         raise ValueError("one source word per destination word")
     _check_pool(pool, params)
     _check(lib.graphattn_kv_copy(_dev_ptr(pool), _dev_ptr(src_words), _dev_ptr(dst_words), n,
-                                 ctypes.byref(params), _stream_handle(stream)))
+                                 ctypes.byref(params), _stream_handle(stream, pool)))
 
 
 def kv_read(pool, slot_words, params: Params, k_out=None, v_out=None, stream=None):
     """graphattn_kv_read: the K and V of the tokens at slot_words, (k [n, Hkv, D], v [n, Hkv, D]);
     rows of words outside the pool are left as they were (zero where this call allocates)."""
-    import torch
+    torch = _torch or _load_torch()
     lib = load_library()
     n = int(slot_words.numel())
     shape = (n, params.num_kv_heads, params.head_dim)
@@ -326,13 +331,13 @@ def kv_read(pool, slot_words, params: Params, k_out=None, v_out=None, stream=Non
         k_out = torch.zeros(shape, dtype=dt, device=pool.device)
     if v_out is None:
         v_out = torch.zeros(shape, dtype=dt, device=pool.device)
-    if tuple(k_out.shape) != shape or tuple(v_out.shape) != shape:
+    if k_out.shape != shape or v_out.shape != shape:
         raise ValueError("one K row and one V row [Hkv, D] per slot word")
     if k_out.dtype != dt or v_out.dtype != dt or slot_words.dtype != torch.int32:
         raise ValueError(f"k_out and v_out must be {dt}, slot_words int32")
     _check_pool(pool, params)
     _check(lib.graphattn_kv_read(_dev_ptr(pool), _dev_ptr(slot_words), n, _dev_ptr(k_out),
-                                 _dev_ptr(v_out), ctypes.byref(params), _stream_handle(stream)))
+                                 _dev_ptr(v_out), ctypes.byref(params), _stream_handle(stream, pool)))
     return k_out, v_out
 
 
@@ -515,7 +520,7 @@ class Plan:
     def run(self, q, pool, out, lse, stream=None):
         _check_pool(pool, self.params, q)
         _check(self.lib.graphattn_run(self.handle, _dev_ptr(q), _dev_ptr(pool), _dev_ptr(out),
-                                      _dev_ptr(lse), _stream_handle(stream)))
+                                      _dev_ptr(lse), _stream_handle(stream, pool)))
 
     def run_mass(self, q, pool, lse, mass_out, mass_in=None, decay: float = 1.0, stream=None):
         """graphattn_run_mass: the attention weight every cached token received from these rows
@@ -533,7 +538,7 @@ class Plan:
             raise ValueError("lse and the masses must be float32")
         _check(self.lib.graphattn_run_mass(self.handle, _dev_ptr(q), _dev_ptr(pool), _dev_ptr(lse),
                                            _dev_ptr(mass_in), float(decay), _dev_ptr(mass_out),
-                                           _stream_handle(stream)))
+                                           _stream_handle(stream, pool)))
         return mass_out
 
     def info(self) -> PlanInfo:
@@ -630,7 +635,7 @@ class Evict:
         if self.total:
             _check(self.lib.graphattn_evict_select(self.handle, _dev_ptr(mass),
                                                    _dev_ptr(positions), _dev_ptr(slot_words),
-                                                   _stream_handle(stream)))
+                                                   _stream_handle(stream, mass)))
         return positions, slot_words
 
     def close(self):

@@ -190,3 +190,28 @@ def test_binding_refuses_tensors_of_other_types_and_sizes():
     g = G.HostGraph([20], [0, 2], [0, 1], [0, 1], [0])
     with pytest.raises(ValueError, match="bf16"):
         G.decode_static(torch.zeros(1, 4, 64), pool, g, p, None, None)
+
+
+def test_binding_refuses_a_tensor_of_another_device(monkeypatch):
+    """Where no stream is given: the call would go to the current device's."""
+    torch = pytest.importorskip("torch")
+
+    class Far:
+        dtype, is_cuda, shape = torch.int32, True, (2, 2, 64)
+
+        def get_device(self):
+            return 1
+
+        def numel(self):
+            return 2
+
+        def is_contiguous(self):
+            return True
+
+        def data_ptr(self):
+            return 1 << 20
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    p, t = G.make_params(4, 2, 64, 3, "bf16"), Far()
+    for call in (lambda: G.kv_append(t, t, t, t, p), lambda: G.kv_copy(t, t, t, p)):
+        with pytest.raises(ValueError, match="device 1"):
+            call()
