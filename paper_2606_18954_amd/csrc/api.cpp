@@ -345,8 +345,12 @@ void size_schedule(const ga_segment_table* st, const ga_branch_paths* bp, const 
   // its first page, so short units pay mostly overhead, unless the graph is too small to give
   // every workgroup work (then short chunks spread it; 4 pages at the least).  Fewer, longer
   // chunks also mean fewer partial rows to merge and fewer items to schedule.
+  // An MXFP4 decode step, whose pages take less of a unit's time, gets 3 (us, 4 | 3: 4 prompts' branches of 8000
+  // tokens, 40/8 heads 52.5 | 44.7, 30 chains of 3000 37.1 | 34.2, 8 merged graphs 75.5 | 73.5; with 28/4
+  // heads 53.5 | 55.1; 2 gave the last 59.6).
+  const bool fp4 = p->dtype == GA_MXFP4;
   const int64_t wgs = 2LL * num_cus;
-  const int64_t target_items = 4 * wgs;
+  const int64_t target_items = (fp4 && !multi_query ? 3 : 4) * wgs;
   // Multi-query plans whose pages are read for many rows run mq_attn.hpp, whose four waves each own
   // 32 rows of a block.  Its units are sized by the pages of every row block (each is a unit), and
   // not cut below 16 pages, so that short prompts keep one partial per row and need no merge.  The
@@ -361,7 +365,6 @@ void size_schedule(const ga_segment_table* st, const ga_branch_paths* bp, const 
   // 49 | 51, 4 queries (70 rows) 56 | 54; one tree of 40/8 heads, 4 queries (50 rows) 30 | 18; from 64 on
   // merged DAGs of 24 prompts, 4 queries (112 rows) 221 | 241, 8 queries (224 rows) 366 | 324; 12/12
   // heads x 64, 16 queries (64 rows) 313 | 446.
-  const bool fp4 = p->dtype == GA_MXFP4;
   const bool full = block_pages * p->num_kv_heads >= 64 * wgs;
   const bool many_rows =
       multi_query &&
