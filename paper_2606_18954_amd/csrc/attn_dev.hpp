@@ -31,14 +31,21 @@ namespace {
 // The multi-query (causal) variant copies with the normal cache policy instead: there the row
 // blocks of one chunk read the same pages, and the later ones find them in the caches.
 // (tests/test_isa_invariants.py checks in the built assembly that every M0 write is one of these.)
+// A copy reads M0 one wait state after a scalar write of it at the earliest: without one it may still see the
+// value before, and its 1 KiB lands where the copy before it went (a work item's page words and branch ids
+// would then be another item's, or whatever LDS held).  The compiler's hazard checks do not look inside inline
+// assembly, so the wait state stands here: 0xbf800000 is s_nop 0, as a word, so that the copy stays the
+// assembly's next instruction by name for the test above; tests/test_isa_wait_states.py checks the machine
+// code.
+#define GA_M0_WAIT ".long 0xbf800000\n\t"
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void dma16(unsigned off, const void* base, unsigned lds_base) {
-  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1 nt"
+  asm volatile("s_mov_b32 m0, %2\n\t" GA_M0_WAIT "global_load_lds_dwordx4 %0, %1 nt"
                :: "v"(off), "s"(base), "s"(lds_base) : "memory", "m0");
 }
 __device__ __forceinline__ void dma16_cached(unsigned off, const void* base, unsigned lds_base) {
-  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1"
+  asm volatile("s_mov_b32 m0, %2\n\t" GA_M0_WAIT "global_load_lds_dwordx4 %0, %1"
                :: "v"(off), "s"(base), "s"(lds_base) : "memory", "m0");
 }
 // Partial-row stores with device scope (sc1): the L2 writes them through to the memory side at

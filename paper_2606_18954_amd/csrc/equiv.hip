@@ -358,7 +358,7 @@ struct TCfg {
 #pragma clang diagnostic ignored "-Winline-asm"
 // The same copy from a 64-bit address per lane (rows of any width).
 __device__ __forceinline__ void dma16_at(const void* p, unsigned lds_base) {
-  asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off"
+  asm volatile("s_mov_b32 m0, %1\n\t" GA_M0_WAIT "global_load_lds_dwordx4 %0, off"
                :: "v"(p), "s"(lds_base) : "memory", "m0");
 }
 #pragma clang diagnostic pop
