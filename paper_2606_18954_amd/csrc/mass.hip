@@ -345,6 +345,11 @@ __global__ __launch_bounds__(64 * mass_wg_waves(D, KIND), mass_waves(D, TYPE, KI
           float nl[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) nl[i] = __shfl(nr, 4 * kg + i);
+          // (masked last: a row whose lse is NaN says nothing of a token that it does not see)
+#pragma unroll
+          for (int g = 0; g < C::PG; ++g)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) S[g][i] = fmaf(S[g][i], a.scale_log2, nl[i]);
           if (cm) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -355,12 +360,8 @@ __global__ __launch_bounds__(64 * mass_wg_waves(D, KIND), mass_waves(D, TYPE, KI
             }
           }
 #pragma unroll
-          for (int g = 0; g < C::PG; ++g) {
-            float e[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) e[i] = exp2_(fmaf(S[g][i], a.scale_log2, nl[i]));
-            acc[g] += (e[0] + e[1]) + (e[2] + e[3]);
-          }
+          for (int g = 0; g < C::PG; ++g)
+            acc[g] += (exp2_(S[g][0]) + exp2_(S[g][1])) + (exp2_(S[g][2]) + exp2_(S[g][3]));
 #pragma unroll
           for (int s = 0; s < C::OPS; ++s) qo[s] = qn[s];
           l0 = l1;

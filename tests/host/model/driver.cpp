@@ -175,8 +175,9 @@ struct Case {
 
 struct Result { std::vector<double> out, lse, bound, lse_bound, mass, mass_bound; };
 
-// out, lse and the masses of the rows, in 64 bits; q [rows][Hq][D].
-Result reference(const Case& c, const Pool& pool, const std::vector<double>& q) {
+// out, lse and the masses of the rows, in 64 bits; q [rows][Hq][D].  odd [rows][Hq]: an lse to gather the masses
+// with in place of the row's own, where it is not 0.
+Result reference(const Case& c, const Pool& pool, const std::vector<double>& q, const std::vector<double>& odd) {
   const int Hq = c.p.num_q_heads, G = Hq / c.p.num_kv_heads, D = c.p.head_dim;
   Result r;
   r.mass.assign((size_t)(16 * c.p.num_pages), 0.);
@@ -210,7 +211,9 @@ Result reference(const Case& c, const Pool& pool, const std::vector<double>& q) 
         for (size_t t = 0; t < n; ++t) {
           const double e = std::exp(s[t] - lse);
           const int64_t slot = c.ctx[b][t];
-          r.mass[slot] += e;
+          const double given = odd[row * Hq + h];
+          // (an infinite lse: the row counts for nothing; NaN: for every token that it sees, and no other)
+          r.mass[slot] += given == 0. ? e : std::isnan(given) ? NAN : 0.;
           r.mass_bound[slot] += e * ((D + 8) * std::ldexp(1., -24) * reach[t] +
                                      std::ldexp(1., -22) * (2. + reach[t] + std::fabs(lse)) + std::ldexp(1., -16));
           const double* v = &pool.v[1][pool.at(slot, h / G, 0)];
@@ -231,8 +234,8 @@ void compare(const char* what, const std::vector<double>& got, const std::vector
              const std::vector<double>& bound) {
   double worst = 0.;
   for (size_t i = 0; i < want.size(); ++i) {
-    const double d = std::fabs(got[i] - want[i]);
-    if (!(d <= bound[i])) {
+    const double d = std::isnan(want[i]) && std::isnan(got[i]) ? 0. : std::fabs(got[i] - want[i]);
+    if (!(d <= bound[i] || (d == 0. && std::isnan(want[i])))) {
       std::fprintf(stderr, "%s[%zu]: %g, not %g (off %g, may be %g)\n", what, i, got[i], want[i], d, bound[i]);
       std::exit(1);
     }
@@ -279,7 +282,10 @@ void attend(bool mass_of_it, int number) {
   ga_plan* plan = nullptr;
   if (c.many) must(graphattn_plan_create_extend(&st, &bp, c.g.counts.data(), &c.p, nullptr, &plan), "plan");
   else must(graphattn_plan_create(&st, &bp, &c.p, nullptr, &plan), "plan");
-  Result want = reference(c, pool, q);
+  std::vector<double> odd(nq, 0.);
+  if (mass_of_it && U(0, 2) == 0)
+    for (int i = U(1, 3); i > 0; --i) odd[U(0, (int)nq - 1)] = U(0, 2) ? NAN : U(0, 1) ? INFINITY : -INFINITY;
+  Result want = reference(c, pool, q, odd);
   for (int pass = 0; pass < 2; ++pass) {
     emu::late_copies = pass;
     emu::seed = 88172645463325252ull + 2 * rng() + 1;
@@ -294,7 +300,7 @@ void attend(bool mass_of_it, int number) {
       compare("lse", l, want.lse, want.lse_bound);
     } else {
       Dev<float> lse(nq), in((size_t)(16 * c.g.num_pages)), out((size_t)(16 * c.g.num_pages));
-      for (size_t i = 0; i < nq; ++i) lse[i] = (float)want.lse[i];
+      for (size_t i = 0; i < nq; ++i) lse[i] = (float)(odd[i] != 0. ? odd[i] : want.lse[i]);
       for (size_t i = 0; i < in.n; ++i) { in[i] = (float)U(0, 9); out[i] = -7.f; }
       const bool with = U(0, 2);
       must(graphattn_run_mass(plan, dq.p, pool.mem.p, lse.p, with ? in.p : nullptr, 0.5f, out.p, nullptr), "mass");
@@ -319,7 +325,7 @@ void attend(bool mass_of_it, int number) {
       for (const auto& x : c.ctx)
         for (int64_t s : x)
           if (!used[s]) { used[s] = 1; pool.put(s); }
-      want = reference(c, pool, q);
+      want = reference(c, pool, q, odd);
     }
   }
   ga_plan_info info;
