@@ -187,8 +187,11 @@ class HostGraph:
 
 def make_params(num_q_heads: int, num_kv_heads: int, head_dim: int, num_pages: int, dtype: str,
                 softmax_scale: float = 0.0, out_f32: bool = False) -> Params:
+    """dtype: of the pool, "f32", "bf16" or "mxfp4"."""
+    if dtype not in DTYPES:
+        raise ValueError(f"dtype {dtype!r} is none of {', '.join(DTYPES)}")
     return Params(num_q_heads, num_kv_heads, head_dim, 16, num_pages,
-                  DTYPES.get(dtype, GA_F32), softmax_scale, int(bool(out_f32)))
+                  DTYPES[dtype], softmax_scale, int(bool(out_f32)))
 
 
 _torch = None
