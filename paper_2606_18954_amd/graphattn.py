@@ -3,6 +3,11 @@
 Every step of the computation runs in the HIP library; this module only turns numpy index arrays
 and torch device tensors into the C ABI's structs and pointers.  If the library is not built, or
 the process has no GPU, the compute entry points raise instead of falling back to anything.
+
+Tensors are contiguous and on one device.  The calls that take a pool check the element types of the pool,
+of the rows beside it and of slot words, lse and masses, and that each holds what the call reads or writes
+(about a microsecond a call); ValueError otherwise.  Without a stream a call goes to the current stream of
+the current device, and a pool (or mass) of another device is refused.
 """
 from __future__ import annotations
 
@@ -231,18 +236,71 @@ def _dev_ptr(t) -> int:
     return int(t.data_ptr())
 
 
-def _check_pool(pool, params: Params, *rows):
-    """An MXFP4 pool's bytes (uint8) hold its pages, and q, K and V rows beside it are bf16: tensors of another
-    layout would be read past their end."""
-    if params.dtype != GA_MXFP4:
-        return
+_LAYOUTS = None
+
+
+def _layouts() -> dict:
+    """By type: a pool's element type, its values per page, kv-head and channel, the type of q, K and V rows and
+    its name, and what a message calls the pool."""
+    global _LAYOUTS
     torch = _torch or _load_torch()
-    if pool.dtype != torch.uint8 or \
-            pool.numel() < 17 * params.head_dim * params.num_kv_heads * params.num_pages:
-        raise ValueError("an MXFP4 pool is a uint8 tensor [num_pages, Hkv, 17 D]")
+    pages = "tensor [num_pages, Hkv, 2, 16, D]"
+    _LAYOUTS = {GA_F32: (torch.float32, 32, torch.float32, "f32", "an f32 pool is a float32 " + pages),
+                GA_BF16: (torch.bfloat16, 32, torch.bfloat16, "bf16", "a bf16 pool is a bfloat16 " + pages),
+                GA_MXFP4: (torch.uint8, 17, torch.bfloat16, "bf16",
+                           "an MXFP4 pool is a uint8 tensor [num_pages, Hkv, 17 D]")}
+    return _LAYOUTS
+
+
+def _layout(params: Params):
+    """(element type, values, type of the rows, its name, description) of a pool."""
+    known = (_LAYOUTS or _layouts()).get(params.dtype)
+    if known is None:                                # (the library refuses the type)
+        return None
+    element, values, row, name, what = known
+    return element, values * params.head_dim * params.num_kv_heads * params.num_pages, row, name, what
+
+
+def _row_sizes(params: Params, rows: int) -> tuple:
+    """(values of q and out, values of lse, whether out is float32) of an attention call."""
+    n = rows * params.num_q_heads
+    return n * params.head_dim, n, bool(params.out_f32)
+
+
+def _enter(stream, pool, layout, *rows) -> int:
+    """Handle of a call's stream, once its pool and the q, K and V rows beside it are what its params say:
+    tensors of another layout would be read, or written, past their end."""
+    if pool is None or layout is None:               # (refused by the library)
+        return _stream_handle(stream)
+    # (a tensor of the host is refused where its pointer is taken)
+    handle = _stream_handle(stream, pool) if pool.is_cuda else 0
+    element, values, row, name, what = layout
+    if pool.dtype != element or pool.numel() < values:
+        raise ValueError(what)
     for t in rows:
-        if t.dtype != torch.bfloat16:
-            raise ValueError("q, K and V rows of an MXFP4 pool are bf16")
+        if t is not None and t.dtype != row:
+            raise ValueError(f"q, K and V rows beside this pool are {name}; {what}")
+    return handle
+
+
+def _check_rows(sizes: tuple, q, out, lse):
+    """q, out and lse of an attention call."""
+    values, n, wide = sizes
+    if q is not None and q.numel() < values:
+        raise ValueError("one row [Hq, D] of q per query")
+    if out is not None:
+        if out.dtype != (_torch.float32 if wide or q is None else q.dtype):
+            raise ValueError("out must be float32 with out_f32, else of q's type")
+        if out.numel() < values:
+            raise ValueError("one row [Hq, D] of out per query")
+    if lse is not None and (lse.dtype != _torch.float32 or lse.numel() < n):
+        raise ValueError("lse must be float32, one row [Hq] per query")
+
+
+def _check_words(*words):
+    for t in words:
+        if t.dtype != _torch.int32:
+            raise ValueError("slot words must be int32")
 
 
 def decode(q, pool, graph: HostGraph, params: Params, out=None, lse=None, stream=None):
@@ -255,10 +313,11 @@ def decode(q, pool, graph: HostGraph, params: Params, out=None, lse=None, stream
         out = torch.empty((B, params.num_q_heads, params.head_dim), dtype=odt, device=q.device)
     if lse is None:
         lse = torch.empty((B, params.num_q_heads), dtype=torch.float32, device=q.device)
-    _check_pool(pool, params, q)
+    handle = _enter(stream, pool, _layout(params), q)
+    _check_rows(_row_sizes(params, B), q, out, lse)
     _check(lib.graphattn_decode(_dev_ptr(q), _dev_ptr(pool), ctypes.byref(graph.st),
                                 ctypes.byref(graph.bp), _dev_ptr(out), _dev_ptr(lse),
-                                ctypes.byref(params), _stream_handle(stream, pool)))
+                                ctypes.byref(params), handle))
     return out, lse
 
 
@@ -266,10 +325,11 @@ def decode_static(q, pool, graph: HostGraph, params: Params, out, lse, stream=No
     """graphattn_decode_static: graphattn_decode with its workspace in the library's static
     device array (no allocation; the caller passes out and lse)."""
     lib = load_library()
-    _check_pool(pool, params, q)
+    handle = _enter(stream, pool, _layout(params), q)
+    _check_rows(_row_sizes(params, graph.bp.num_branches), q, out, lse)
     _check(lib.graphattn_decode_static(_dev_ptr(q), _dev_ptr(pool), ctypes.byref(graph.st),
                                        ctypes.byref(graph.bp), _dev_ptr(out), _dev_ptr(lse),
-                                       ctypes.byref(params), _stream_handle(stream, pool)))
+                                       ctypes.byref(params), handle))
     return out, lse
 
 
@@ -292,10 +352,11 @@ def extend(q, pool, graph: HostGraph, query_counts, params: Params, out=None, ls
         out = torch.empty((R, params.num_q_heads, params.head_dim), dtype=odt, device=q.device)
     if lse is None:
         lse = torch.empty((R, params.num_q_heads), dtype=torch.float32, device=q.device)
-    _check_pool(pool, params, q)
+    handle = _enter(stream, pool, _layout(params), q)
+    _check_rows(_row_sizes(params, R), q, out, lse)
     _check(lib.graphattn_extend(_dev_ptr(q), _dev_ptr(pool), ctypes.byref(graph.st),
                                 ctypes.byref(graph.bp), _ptr(cnt, ctypes.c_int32), _dev_ptr(out),
-                                _dev_ptr(lse), ctypes.byref(params), _stream_handle(stream, pool)))
+                                _dev_ptr(lse), ctypes.byref(params), handle))
     return out, lse
 
 
@@ -305,10 +366,13 @@ def kv_append(pool, k_new, v_new, slot_words, params: Params, stream=None):
     n = int(slot_words.numel())
     if k_new.shape[0] != n or v_new.shape[0] != n:
         raise ValueError("one K row and one V row per slot word")
-    _check_pool(pool, params, k_new, v_new)
+    handle = _enter(stream, pool, _layout(params), k_new, v_new)
+    _check_words(slot_words)
+    size = n * params.num_kv_heads * params.head_dim
+    if k_new.numel() < size or v_new.numel() < size:
+        raise ValueError("K and V rows are [Hkv, D]")
     _check(lib.graphattn_kv_append(_dev_ptr(pool), _dev_ptr(k_new), _dev_ptr(v_new),
-                                   _dev_ptr(slot_words), n, ctypes.byref(params),
-                                   _stream_handle(stream, pool)))
+                                   _dev_ptr(slot_words), n, ctypes.byref(params), handle))
 
 
 def kv_copy(pool, src_words, dst_words, params: Params, stream=None):
@@ -317,9 +381,10 @@ def kv_copy(pool, src_words, dst_words, params: Params, stream=None):
     n = int(dst_words.numel())
     if src_words.numel() != n:
         raise ValueError("one source word per destination word")
-    _check_pool(pool, params)
+    handle = _enter(stream, pool, _layout(params))
+    _check_words(src_words, dst_words)
     _check(lib.graphattn_kv_copy(_dev_ptr(pool), _dev_ptr(src_words), _dev_ptr(dst_words), n,
-                                 ctypes.byref(params), _stream_handle(stream, pool)))
+                                 ctypes.byref(params), handle))
 
 
 def kv_read(pool, slot_words, params: Params, k_out=None, v_out=None, stream=None):
@@ -338,9 +403,9 @@ def kv_read(pool, slot_words, params: Params, k_out=None, v_out=None, stream=Non
         raise ValueError("one K row and one V row [Hkv, D] per slot word")
     if k_out.dtype != dt or v_out.dtype != dt or slot_words.dtype != torch.int32:
         raise ValueError(f"k_out and v_out must be {dt}, slot_words int32")
-    _check_pool(pool, params)
+    handle = _enter(stream, pool, _layout(params))
     _check(lib.graphattn_kv_read(_dev_ptr(pool), _dev_ptr(slot_words), n, _dev_ptr(k_out),
-                                 _dev_ptr(v_out), ctypes.byref(params), _stream_handle(stream, pool)))
+                                 _dev_ptr(v_out), ctypes.byref(params), handle))
     return k_out, v_out
 
 
@@ -506,7 +571,13 @@ class Plan:
                 _stream_handle(stream), ctypes.byref(h)))
         self.handle = h
         # query rows of a run
-        self.rows = int(graph.bp.num_branches if query_counts is None else self.query_counts.sum())
+        self._keep(params, int(graph.bp.num_branches if query_counts is None else self.query_counts.sum()))
+
+    def _keep(self, params: Params, rows: int):
+        """What the plan's calls are checked against (the library has its own copy of the params)."""
+        self.rows = rows
+        self.layout = _layout(params)
+        self.sizes = _row_sizes(params, rows)
 
     def set_lengths(self, seg_len, stream=None):
         """New segment lengths (host int32 [num_segments]); schedule again before the next run."""
@@ -521,27 +592,25 @@ class Plan:
         _check(self.lib.graphattn_schedule(self.handle, _stream_handle(stream)))
 
     def run(self, q, pool, out, lse, stream=None):
-        _check_pool(pool, self.params, q)
+        handle = _enter(stream, pool, self.layout, q)
+        _check_rows(self.sizes, q, out, lse)
         _check(self.lib.graphattn_run(self.handle, _dev_ptr(q), _dev_ptr(pool), _dev_ptr(out),
-                                      _dev_ptr(lse), _stream_handle(stream, pool)))
+                                      _dev_ptr(lse), handle))
 
     def run_mass(self, q, pool, lse, mass_out, mass_in=None, decay: float = 1.0, stream=None):
         """graphattn_run_mass: the attention weight every cached token received from these rows
         (lse as run() wrote it), added to decay x mass_in (float32 [num_pages x 16])."""
-        import torch
-        p = self.params
-        _check_pool(pool, p, q)
-        if q.numel() < self.rows * p.num_q_heads * p.head_dim or \
-                lse.numel() < self.rows * p.num_q_heads:
+        handle = _enter(stream, pool, self.layout, q)
+        if q.numel() < self.sizes[0] or lse.numel() < self.sizes[1]:
             raise ValueError("one row of q and of lse per query")
         for t in (mass_out, mass_in):
-            if t is not None and t.numel() < 16 * p.num_pages:
+            if t is not None and t.numel() < 16 * self.params.num_pages:
                 raise ValueError("one mass per slot of the pool")
-        if any(t is not None and t.dtype != torch.float32 for t in (lse, mass_out, mass_in)):
+        if any(t is not None and t.dtype != _torch.float32 for t in (lse, mass_out, mass_in)):
             raise ValueError("lse and the masses must be float32")
         _check(self.lib.graphattn_run_mass(self.handle, _dev_ptr(q), _dev_ptr(pool), _dev_ptr(lse),
                                            _dev_ptr(mass_in), float(decay), _dev_ptr(mass_out),
-                                           _stream_handle(stream, pool)))
+                                           handle))
         return mass_out
 
     def info(self) -> PlanInfo:
