@@ -32,6 +32,9 @@ ga_status graphattn_kv_read(const void* kv_page_pool, const int32_t* slot_words,
  * chosen by it (graphattn_evict_select), moved to fresh pages (graphattn_kv_copy with the chosen slot
  * words as sources) and the segment goes on with its new length and pages.  Keys are stored with their
  * positions applied, so the tokens that stay attend as before.
+ * The mass belongs to the slot, and no call here moves or clears it: after the move mass[new word] =
+ * mass[kept word] for every token that stayed, and a slot that takes a new token (graphattn_kv_append) is
+ * set to 0, or that token goes on from what the slot's last one had gathered.
  *
  * graphattn_run_mass: for every slot w of the tokens of the plan's chains (segments on some path, at
  * their current lengths)

@@ -599,7 +599,8 @@ class Plan:
 
     def run_mass(self, q, pool, lse, mass_out, mass_in=None, decay: float = 1.0, stream=None):
         """graphattn_run_mass: the attention weight every cached token received from these rows
-        (lse as run() wrote it), added to decay x mass_in (float32 [num_pages x 16])."""
+        (lse as run() wrote it), added to decay x mass_in (float32 [num_pages x 16]).  A slot's mass does
+        not move with its token (kv_copy), and is not cleared for a new one (kv_append): the caller does both."""
         handle = _enter(stream, pool, self.layout, q)
         if q.numel() < self.sizes[0] or lse.numel() < self.sizes[1]:
             raise ValueError("one row of q and of lse per query")
