@@ -252,10 +252,11 @@ def _layouts() -> dict:
     return _LAYOUTS
 
 
-def _layout(params: Params):
-    """(element type, values, type of the rows, its name, description) of a pool."""
+def _layout(params: Params, n: int):
+    """(element type, values, type of the rows, its name, description) of the pool of a call with n rows or
+    tokens; None where there is nothing to check."""
     known = (_LAYOUTS or _layouts()).get(params.dtype)
-    if known is None:                                # (the library refuses the type)
+    if known is None or n == 0:                      # (refused by the library; nothing is read or written)
         return None
     element, values, row, name, what = known
     return element, values * params.head_dim * params.num_kv_heads * params.num_pages, row, name, what
@@ -270,8 +271,8 @@ def _row_sizes(params: Params, rows: int) -> tuple:
 def _enter(stream, pool, layout, *rows) -> int:
     """Handle of a call's stream, once its pool and the q, K and V rows beside it are what its params say:
     tensors of another layout would be read, or written, past their end."""
-    if pool is None or layout is None:               # (refused by the library)
-        return _stream_handle(stream)
+    if pool is None or layout is None:               # (no pool: refused by the library)
+        return _stream_handle(stream, pool) if pool is not None and pool.is_cuda else _stream_handle(stream)
     # (a tensor of the host is refused where its pointer is taken)
     handle = _stream_handle(stream, pool) if pool.is_cuda else 0
     element, values, row, name, what = layout
@@ -313,7 +314,7 @@ def decode(q, pool, graph: HostGraph, params: Params, out=None, lse=None, stream
         out = torch.empty((B, params.num_q_heads, params.head_dim), dtype=odt, device=q.device)
     if lse is None:
         lse = torch.empty((B, params.num_q_heads), dtype=torch.float32, device=q.device)
-    handle = _enter(stream, pool, _layout(params), q)
+    handle = _enter(stream, pool, _layout(params, B), q)
     _check_rows(_row_sizes(params, B), q, out, lse)
     _check(lib.graphattn_decode(_dev_ptr(q), _dev_ptr(pool), ctypes.byref(graph.st),
                                 ctypes.byref(graph.bp), _dev_ptr(out), _dev_ptr(lse),
@@ -325,7 +326,7 @@ def decode_static(q, pool, graph: HostGraph, params: Params, out, lse, stream=No
     """graphattn_decode_static: graphattn_decode with its workspace in the library's static
     device array (no allocation; the caller passes out and lse)."""
     lib = load_library()
-    handle = _enter(stream, pool, _layout(params), q)
+    handle = _enter(stream, pool, _layout(params, graph.bp.num_branches), q)
     _check_rows(_row_sizes(params, graph.bp.num_branches), q, out, lse)
     _check(lib.graphattn_decode_static(_dev_ptr(q), _dev_ptr(pool), ctypes.byref(graph.st),
                                        ctypes.byref(graph.bp), _dev_ptr(out), _dev_ptr(lse),
@@ -352,7 +353,7 @@ def extend(q, pool, graph: HostGraph, query_counts, params: Params, out=None, ls
         out = torch.empty((R, params.num_q_heads, params.head_dim), dtype=odt, device=q.device)
     if lse is None:
         lse = torch.empty((R, params.num_q_heads), dtype=torch.float32, device=q.device)
-    handle = _enter(stream, pool, _layout(params), q)
+    handle = _enter(stream, pool, _layout(params, R), q)
     _check_rows(_row_sizes(params, R), q, out, lse)
     _check(lib.graphattn_extend(_dev_ptr(q), _dev_ptr(pool), ctypes.byref(graph.st),
                                 ctypes.byref(graph.bp), _ptr(cnt, ctypes.c_int32), _dev_ptr(out),
@@ -366,7 +367,7 @@ def kv_append(pool, k_new, v_new, slot_words, params: Params, stream=None):
     n = int(slot_words.numel())
     if k_new.shape[0] != n or v_new.shape[0] != n:
         raise ValueError("one K row and one V row per slot word")
-    handle = _enter(stream, pool, _layout(params), k_new, v_new)
+    handle = _enter(stream, pool, _layout(params, n), k_new, v_new)
     _check_words(slot_words)
     size = n * params.num_kv_heads * params.head_dim
     if k_new.numel() < size or v_new.numel() < size:
@@ -381,7 +382,7 @@ def kv_copy(pool, src_words, dst_words, params: Params, stream=None):
     n = int(dst_words.numel())
     if src_words.numel() != n:
         raise ValueError("one source word per destination word")
-    handle = _enter(stream, pool, _layout(params))
+    handle = _enter(stream, pool, _layout(params, n))
     _check_words(src_words, dst_words)
     _check(lib.graphattn_kv_copy(_dev_ptr(pool), _dev_ptr(src_words), _dev_ptr(dst_words), n,
                                  ctypes.byref(params), handle))
@@ -403,7 +404,7 @@ def kv_read(pool, slot_words, params: Params, k_out=None, v_out=None, stream=Non
         raise ValueError("one K row and one V row [Hkv, D] per slot word")
     if k_out.dtype != dt or v_out.dtype != dt or slot_words.dtype != torch.int32:
         raise ValueError(f"k_out and v_out must be {dt}, slot_words int32")
-    handle = _enter(stream, pool, _layout(params))
+    handle = _enter(stream, pool, _layout(params, n))
     _check(lib.graphattn_kv_read(_dev_ptr(pool), _dev_ptr(slot_words), n, _dev_ptr(k_out),
                                  _dev_ptr(v_out), ctypes.byref(params), handle))
     return k_out, v_out
@@ -576,7 +577,7 @@ class Plan:
     def _keep(self, params: Params, rows: int):
         """What the plan's calls are checked against (the library has its own copy of the params)."""
         self.rows = rows
-        self.layout = _layout(params)
+        self.layout = _layout(params, rows)
         self.sizes = _row_sizes(params, rows)
 
     def set_lengths(self, seg_len, stream=None):
