@@ -60,7 +60,7 @@ typedef enum {
  * "MXFP4 pools" below). */
 typedef enum { GA_F32 = 0, GA_BF16 = 1, GA_MXFP4 = 2 } ga_dtype;
 
-/* MXFP4 pools (a quarter of bf16's bytes: 4.25 bits a value).  Each block of 32 channels of one
+/* MXFP4 pools (17/64 of bf16's bytes: 4.25 bits a value; graphattn_kv_page_bytes).  Each block of 32 channels of one
  * token's K or V shares a power of two: byte E, scale 2^(E - 127) (E = 255: every value of the block
  * is NaN).  A value is a 4-bit code: bit 3 the sign, bits 0..2 one of 0, 0.5, 1, 1.5, 2, 3, 4, 6, times
  * the block's scale.  Appending rounds a block with largest magnitude a to e = floor(log2 a) - 2, plus

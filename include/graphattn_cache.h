@@ -1,6 +1,6 @@
 /*
  * graphattn_cache.h -- holding longer rollouts in the same pool: reading tokens back from a page pool
- * (MXFP4 pools hold four times the tokens of bf16 ones; ga_dtype in graphattn.h), the attention mass of
+ * (MXFP4 pools hold 64/17 = 3.76 times the tokens of bf16 ones; ga_dtype in graphattn.h), the attention mass of
  * cached tokens, and the choice of the tokens that stay when a segment gives up the others.
  *
  * Conventions, errors and streams as in graphattn.h.

@@ -360,7 +360,7 @@ void size_schedule(const ga_segment_table* st, const ga_branch_paths* bp, const 
   // workgroup) 38.6 | 42.2, 32 queries 121 | 54; merged DAGs of 24 prompts, 2 queries (56 rows, 200
   // pages a workgroup) 249 | 245; 12/12 heads x 64, 8 queries (32 rows) 269.6 | 273.6.  One query per
   // branch stays on the other kernel, whose bits decode has.
-  // MXFP4 pools cross elsewhere: a page is a quarter of the bytes, and mq_attn converts it once for its
+  // MXFP4 pools cross elsewhere: a page is 17/64 of the bytes, and mq_attn converts it once for its
   // block's rows (fp4_attn.hip | mq_attn): under 64 pages a workgroup 16 step trees, 2 queries (35 rows)
   // 49 | 51, 4 queries (70 rows) 56 | 54; one tree of 40/8 heads, 4 queries (50 rows) 30 | 18; from 64 on
   // merged DAGs of 24 prompts, 4 queries (112 rows) 221 | 241, 8 queries (224 rows) 366 | 324; 12/12

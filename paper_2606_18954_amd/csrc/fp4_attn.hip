@@ -5,7 +5,7 @@
 //   S^T = K Q^T   (16 tokens x 16 rows per matrix tile, contraction over head_dim)
 //   O^T += V^T P^T (contraction over the 32 tokens of a pair of pages)
 //
-// A page of a kv-head is 17 D bytes (mxfp4.hpp), a quarter of bf16's, so a page that few rows read
+// A page of a kv-head is 17 D bytes (mxfp4.hpp), 17/64 of bf16's, so a page that few rows read
 // is soon there and the instructions per page matter.  Three things keep them few:
 // * The page goes from global memory into registers, in the lanes that need it: a lane's K
 //   operand is D / 4 consecutive channels of one token (the channels' order in the contraction is

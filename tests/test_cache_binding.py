@@ -99,3 +99,9 @@ def test_rows_of_another_type_or_size_are_refused(params, plan):
                  lambda: G.kv_copy(pool, words, words.long(), p)):
         with pytest.raises(ValueError, match="int32"):
             call()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_an_mxfp4_page_is_17_of_64_of_a_bf16_page(D):
+    pages = {n: G.kv_page_bytes(G.make_params(4, 4, D, 1, n)) for n in ("bf16", "mxfp4")}
+    assert 64 * pages["mxfp4"] == 17 * pages["bf16"]
