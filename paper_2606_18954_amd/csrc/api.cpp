@@ -345,9 +345,11 @@ void size_schedule(const ga_segment_table* st, const ga_branch_paths* bp, const 
   // its first page, so short units pay mostly overhead, unless the graph is too small to give
   // every workgroup work (then short chunks spread it; 4 pages at the least).  Fewer, longer
   // chunks also mean fewer partial rows to merge and fewer items to schedule.
-  // An MXFP4 decode step, whose pages take less of a unit's time, gets 3 (us, 4 | 3: 4 prompts' branches of 8000
-  // tokens, 40/8 heads 52.5 | 44.7, 30 chains of 3000 37.1 | 34.2, 8 merged graphs 75.5 | 73.5; with 28/4
-  // heads 53.5 | 55.1; 2 gave the last 59.6).
+  // An MXFP4 decode step, whose pages take less of a unit's time, gets 3.  Over 48 steps of prompts, trees, merged
+  // graphs and chains drawn from one to 64 prompts, 14 have other chunks by it: they take 0.937 of the time with 4
+  // in the geometric mean, 0.834 to 1.010 (us, 4 | 3: 4 prompts' branches of 8000 tokens, 40/8 heads 51.4 | 42.9,
+  // 3 merged graphs of 12/12 heads x 64 41.9 | 35.0, 30 chains of 3000 tokens 35.9 | 33.2, 8 merged graphs of 28/4
+  // heads 50.9 | 51.4; 2 gave the last 59.6).  The others, long or short, are at a bound of the chunk already.
   const bool fp4 = p->dtype == GA_MXFP4;
   const int64_t wgs = 2LL * num_cus;
   const int64_t target_items = (fp4 && !multi_query ? 3 : 4) * wgs;

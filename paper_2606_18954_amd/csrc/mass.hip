@@ -346,22 +346,27 @@ __global__ __launch_bounds__(64 * mass_wg_waves(D, KIND), mass_waves(D, TYPE, KI
 #pragma unroll
           for (int i = 0; i < 4; ++i) nl[i] = __shfl(nr, 4 * kg + i);
           // (masked last: a row whose lse is NaN says nothing of a token that it does not see)
+          auto add = [&](auto masked) {
+            int lim[4];
+            if constexpr (decltype(masked)::value)
 #pragma unroll
-          for (int g = 0; g < C::PG; ++g)
+              for (int i = 0; i < 4; ++i)
+                lim[i] = cw + __shfl(j0, 4 * kg + i) - kPageTokens * (pg0 + p0) - r16;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) S[g][i] = fmaf(S[g][i], a.scale_log2, nl[i]);
-          if (cm) {
+            for (int g = 0; g < C::PG; ++g) {
+              float e[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int lim = cw + __shfl(j0, 4 * kg + i) - kPageTokens * (pg0 + p0) - r16;
-#pragma unroll
-              for (int g = 0; g < C::PG; ++g)
-                S[g][i] = kPageTokens * g > lim ? -__builtin_huge_valf() : S[g][i];
+              for (int i = 0; i < 4; ++i) {
+                float x = fmaf(S[g][i], a.scale_log2, nl[i]);
+                if constexpr (decltype(masked)::value)
+                  x = kPageTokens * g > lim[i] ? -__builtin_huge_valf() : x;
+                e[i] = exp2_(x);
+              }
+              acc[g] += (e[0] + e[1]) + (e[2] + e[3]);
             }
-          }
-#pragma unroll
-          for (int g = 0; g < C::PG; ++g)
-            acc[g] += (exp2_(S[g][0]) + exp2_(S[g][1])) + (exp2_(S[g][2]) + exp2_(S[g][3]));
+          };
+          if (CAUSAL && cm) add(std::true_type{});
+          else add(std::false_type{});
 #pragma unroll
           for (int s = 0; s < C::OPS; ++s) qo[s] = qn[s];
           l0 = l1;
