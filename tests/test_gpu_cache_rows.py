@@ -49,3 +49,36 @@ def test_a_row_without_an_lse_says_nothing_of_later_tokens(n, D):
     assert (np.abs(got[later] - ref[later]) <= bound[later]).all()
     rest = np.setdiff1d(np.arange(16 * g.num_pages), slots)
     assert (got[rest] == -5).all()
+
+
+@pytest.mark.parametrize("counts", [None, [1, 40, 3]])
+def test_a_grown_plan_has_a_fresh_plans_bits(counts):
+    """Mass of a plan that was given new lengths and of one created with them: small graphs, taken in the same
+    parts, have the same bits."""
+    require_gpu()
+    say(f"[case] mass of a grown and a fresh plan {counts}")
+    rng = np.random.default_rng(59)
+    Hq, Hkv, D = 8, 2, 64
+    lens, paths = [700, 90, 130], [[0, 1], [0, 2], [0]]
+    if counts:
+        lens, paths = W.with_new_steps(lens, paths, counts)
+    g = W.assemble_graph(lens, paths, 6, slack_pages=2)
+    rows = sum(counts) if counts else 3
+    raw = poison_unused(random_pool(rng, g.num_pages, Hkv, D, -2, 1), g)
+    vals, q = C.pool_values(raw), draw_q(rng, rows, Hq, D)
+    lse = torch.from_numpy(C.attention(bits_of(q), vals, g, Hq, Hkv, counts)[1].astype(np.float32)).cuda()
+    p = G.make_params(Hq, Hkv, D, g.num_pages, "mxfp4")
+    short = [max(1, n // 3) for n in lens[:3]] + lens[3:]
+    got = []
+    for start in (lens, short):
+        out = torch.full((16 * g.num_pages,), -5.0, device="cuda")
+        with G.Plan(G.HostGraph(start, g.seg_page_offsets, g.seg_pages, g.path_offsets, g.path_segs), p,
+                    query_counts=counts) as pl:
+            if start is short:
+                pl.schedule()
+                pl.run_mass(q.cuda(), torch.from_numpy(raw).cuda(), lse, torch.zeros_like(out))
+                pl.set_lengths(lens)
+            pl.run_mass(q.cuda(), torch.from_numpy(raw).cuda(), lse, out)
+            torch.cuda.synchronize()
+        got.append(out)
+    assert torch.equal(got[0], got[1])
