@@ -65,7 +65,7 @@ typedef enum { GA_F32 = 0, GA_BF16 = 1, GA_MXFP4 = 2 } ga_dtype;
  * is NaN).  A value is a 4-bit code: bit 3 the sign, bits 0..2 one of 0, 0.5, 1, 1.5, 2, 3, 4, 6, times
  * the block's scale.  Appending rounds a block with largest magnitude a to e = floor(log2 a) - 2, plus
  * one where a >= 7 x 2^e, held in [-125, 125] (E = e + 127; a block of zeros has E = 2), and every
- * value x to the code nearest to x / 2^e, ties to the even code; a block with a NaN or an infinity has
+ * value x to the code nearest to x / 2^e, ties to the even code (6 from 7 x 2^125 on); a block with a NaN or an infinity has
  * E = 255.  Attention reads the values exactly as stored (they are bf16 numbers); nothing else differs
  * from a bf16 pool.
  *   kv_page_pool  [num_pages][Hkv][17 D] bytes, 16-byte aligned.  With t = 0..15 a page's token and c

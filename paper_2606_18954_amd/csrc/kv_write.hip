@@ -18,14 +18,16 @@
 // which rounding to it is as near as to the next one: no value is clipped by more than a rounding),
 // kept in [-125, 125] so that every value of the block is a normal float32; x / 2^e is rounded to the
 // nearest code, ties to the even one, by the conversion instruction.  A block with a NaN or an
-// infinity has scale byte 255 and reads as NaN.  Memory bounds it: 32768 tokens of 8 heads x 128 in random
-// order, 169 MB, append 44.8 us, read 37.2 (4.5 TB/s; a plain copy reaches 5.15 on that card).  In random
-// order V's runs of 4 bytes fill a quarter of the 64-byte pieces that reach memory: the append writes 98 MB where
-// 36 are new, and moves 233 MB in all at 5.1 TB/s.  The
-// bf16 rows pass the caches by (non-temporal), so that a page's lines, which four tokens' V share, stay until
-// all have come: with ordinary loads and stores the two take 96 us, not 82.  Two tokens a thread (82 us) hide
-// the latency of the words better than one (85) and leave a step's 1024 tokens more workgroups than four (a
-// step's append and read 10.4 us, 12.0 with four).
+// infinity has scale byte 255 and reads as NaN.  (Only the largest exponent leaves a value outside: from
+// 7 x 2^125 on it becomes 6 x 2^125.)  Memory bounds it: 32768 tokens of 8 heads x 128, 169 MB and 27 us at
+// 6.2 TB/s, in the order in which a prompt's tokens lie (whole pages, at random places) append 40.1 us, read 30.3,
+// copy 25.8; with every token at a random slot 45.9, 38.3 and 44.3.  There V's runs of 4 bytes fill a quarter of
+// the 64-byte pieces that reach memory: the append writes 98 MB where 36 are new, and moves 233 MB in all at
+// 5.1 TB/s.  (The choices below were measured on random slots.)  The bf16 rows pass the caches by
+// (non-temporal), so that a page's lines, which four tokens' V share, stay until all have come: with ordinary
+// loads and stores append and read take 96 us, not 82.  Two tokens a thread (82 us) hide the latency of the
+// words better than one (85) and leave a step's 1024 tokens more workgroups than four (a step's append and read
+// 10.4 us, 12.0 with four).
 #include "ga_internal.hpp"
 #include "mxfp4.hpp"
 #include "pool_load.hpp"
