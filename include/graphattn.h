@@ -132,7 +132,8 @@ ga_status graphattn_decode(const void* q, const void* kv_page_pool,
  * K/V are already in the pool (graphattn_kv_append).  query_counts[b] = n_b in [1, len(last)]
  * (host array): the queries are the segment's last n_b tokens, query i at position
  * len(last) - n_b + i, seeing every token of the other path segments and tokens 0 .. that
- * position of the newest one (itself included).  With n_b = 1 this is graphattn_decode.
+ * position of the newest one (itself included).  With n_b = 1 this is graphattn_decode.  K of a token that a
+ * row does not see may be anything; its V must be finite (its probability is 0, and 0 times NaN is NaN).
  *   q    [R][Hq][D]  R = sum_b n_b query rows, branch-major, ascending i within a branch
  *   out  [R][Hq][D], lse [R][Hq]  (as for decode, per query row)
  * Rows of one branch share its path's segments with each other and with every branch on them,

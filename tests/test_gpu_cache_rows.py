@@ -82,3 +82,48 @@ def test_a_grown_plan_has_a_fresh_plans_bits(counts):
             torch.cuda.synchronize()
         got.append(out)
     assert torch.equal(got[0], got[1])
+
+
+@pytest.mark.parametrize("step", [3, 40, 300])
+@pytest.mark.parametrize("D", [64, 128])
+def test_keys_behind_a_query_may_be_anything(step, D):
+    """NaN in the keys of each branch's last token: attention and mass of the rows before it are as without,
+    with few rows a page and many."""
+    require_gpu()
+    say(f"[case] NaN keys behind {step} queries, {D} channels")
+    rng = np.random.default_rng(step + D)
+    Hq, Hkv = 12, 2
+    counts = [step, step - 1, max(1, step // 2)]
+    lens, paths = W.with_new_steps([150, 33], [[0], [0, 1], [0]], [step, step, step])
+    g = W.assemble_graph(lens, paths, 6, slack_pages=1)
+    raw = poison_unused(random_pool(rng, g.num_pages, Hkv, D, -2, 1), g)
+    vals, q = C.pool_values(raw), draw_q(rng, sum(counts), Hq, D)
+    bad = raw.copy()
+    for s in range(2, 5):
+        t = lens[s] - 1
+        page = int(g.seg_pages[g.seg_page_offsets[s] + t // 16])
+        for c in range(0, D, 32):
+            bad[page, :, C.scale_place(t % 16, c, D, False)] = 255
+    last = np.cumsum(counts) - 1                           # the rows that see those tokens
+    rest = np.setdiff1d(np.arange(sum(counts)), last)
+    oo, ol, _, _ = C.attention(bits_of(q), vals, g, Hq, Hkv, counts)
+    given = ol.astype(np.float32)
+    given[last] = math.inf                                 # (count for nothing)
+    p = G.make_params(Hq, Hkv, D, g.num_pages, "mxfp4")
+    got = []
+    for pool in (raw, bad):
+        out = torch.zeros(sum(counts), Hq, D, dtype=torch.bfloat16, device="cuda")
+        lse = torch.zeros(sum(counts), Hq, device="cuda")
+        mass = torch.full((16 * g.num_pages,), -5.0, device="cuda")
+        with G.Plan(G.HostGraph.from_graph(g), p, query_counts=counts) as pl:
+            pl.run(q.cuda(), torch.from_numpy(pool).cuda(), out, lse)
+            pl.run_mass(q.cuda(), torch.from_numpy(pool).cuda(), torch.from_numpy(given).cuda(), mass)
+            torch.cuda.synchronize()
+        got.append((bits_of(out)[rest], bits_of(lse)[rest], bits_of(mass)))
+    assert np.isfinite(got[0][0]).all()
+    assert np.array_equal(got[0][0], got[1][0]) and np.array_equal(got[0][1], got[1][1])
+    seen = np.array([int(g.seg_pages[g.seg_page_offsets[s] + (lens[s] - 1) // 16]) * 16 + (lens[s] - 1) % 16
+                     for s in range(2, 5)])
+    others = np.setdiff1d(np.arange(16 * g.num_pages), seen)
+    assert np.array_equal(got[0][2][others], got[1][2][others])
+    assert np.isnan(got[1][2][seen]).all()
