@@ -17,7 +17,8 @@ LIB = os.path.join(PKG, "libgraphattn.so")
 SOURCES = ["api.cpp", "sched.hip", "seg_attn.hip", "mq_attn.hip", "mq_fp4_attn.hip",
            "fp4_attn.hip", "merge.hip", "kv_write.hip",
            "equiv.hip", "equiv_api.cpp", "reward.hip",
-           "mass.hip", "evict.hip", "evict_api.cpp"]
+           "mass.hip", "evict.hip", "evict_api.cpp",
+           "slots.hip", "qkv.hip", "logits.hip", "step_api.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 CFLAGS = [

@@ -877,6 +877,10 @@ void profile_clear(ga_plan* pl) {
 }  // namespace
 
 namespace ga {
+ga_status host_check_params(const ga_params* params) { return validate_params(params); }
+}  // namespace ga
+
+namespace ga {
 
 ga_status plan_mass_args(ga_plan* plan, bool schedule, hipStream_t stream, MassArgs* a,
                          int64_t* rows) {

@@ -62,28 +62,6 @@ __global__ __launch_bounds__(256) void k_kv_write(KvWriteArgs a) {
   *reinterpret_cast<uint4*>(a.pool + slot_offset(dw, h, kv, a.Hkv, a.row_bytes) + 16 * c) = *src;
 }
 
-// The codes of 8 channels from c on, in a page block.
-template <int D>
-__device__ __forceinline__ unsigned load_codes(const unsigned char* blk, int t, int c, bool v) {
-  if constexpr (D == 128) {
-    return *reinterpret_cast<const unsigned*>(blk + fp4_code<D>(t, c, v));
-  } else {
-    // (K: both halves side by side; V: two slices of four channels)
-    const unsigned lo = *reinterpret_cast<const unsigned short*>(blk + fp4_code<D>(t, c, v));
-    const unsigned hi = *reinterpret_cast<const unsigned short*>(blk + fp4_code<D>(t, c + 4, v));
-    return lo | (hi << 16);
-  }
-}
-template <int D>
-__device__ __forceinline__ void store_codes(unsigned char* blk, int t, int c, bool v, unsigned w) {
-  if constexpr (D == 128) {
-    *reinterpret_cast<unsigned*>(blk + fp4_code<D>(t, c, v)) = w;
-  } else {
-    *reinterpret_cast<unsigned short*>(blk + fp4_code<D>(t, c, v)) = (unsigned short)w;
-    *reinterpret_cast<unsigned short*>(blk + fp4_code<D>(t, c + 4, v)) = (unsigned short)(w >> 16);
-  }
-}
-
 // MODE 0: append, 1: copy, 2: read.  A thread takes 8 channels of kPieces tokens' K or V, which D / 8 threads
 // share: each kind of load is issued for all of them before the first is used.
 constexpr int kPieces = 2;
@@ -134,23 +112,7 @@ __global__ __launch_bounds__(256) void k_kv_fp4(KvWriteArgs a) {
     if (!ok[i]) continue;
     if constexpr (MODE == 0) {
       const unsigned w[4] = {x[i][0], x[i][1], x[i][2], x[i][3]};
-      // bf16 magnitudes order like the integers they are.
-      unsigned top = 0;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) top = max(top, max(w[k] & 0x7fffu, (w[k] >> 16) & 0x7fffu));
-      top = max(top, (unsigned)__shfl_xor((int)top, 1));
-      top = max(top, (unsigned)__shfl_xor((int)top, 2));
-      // Exponent of a, plus one from mantissa 0.75 on; two below it is the scale.
-      byte[i] = (unsigned)min(max((int)((top + 0x20u) >> 7) - 2, 2), 252);
-      const float s = __builtin_bit_cast(float, byte[i] << 23);
-      unsigned q = 0;
-      q = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(q, __builtin_bit_cast(bf16x2_t, w[0]), s, 0);
-      q = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(q, __builtin_bit_cast(bf16x2_t, w[1]), s, 1);
-      q = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(q, __builtin_bit_cast(bf16x2_t, w[2]), s, 2);
-      q = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(q, __builtin_bit_cast(bf16x2_t, w[3]), s, 3);
-      const bool nan = top >= 0x7f80u;
-      code[i] = nan ? 0 : q;
-      if (nan) byte[i] = 255;
+      fp4_round(w, &code[i], &byte[i]);
     }
     if constexpr (MODE != 2) {
       unsigned char* dst = block(dw[i], i);

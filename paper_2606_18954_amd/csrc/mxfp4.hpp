@@ -64,6 +64,49 @@ __device__ __forceinline__ float fp4_exp_at(unsigned w, unsigned shift) {
   return __builtin_bit_cast(float, __builtin_amdgcn_ubfe(w, shift, 8) << 23);
 }
 
+// The codes of 8 channels from c on, in a page block.
+template <int D>
+__device__ __forceinline__ unsigned load_codes(const unsigned char* blk, int t, int c, bool v) {
+  if constexpr (D == 128) {
+    return *reinterpret_cast<const unsigned*>(blk + fp4_code<D>(t, c, v));
+  } else {
+    // (K: both halves side by side; V: two slices of four channels)
+    const unsigned lo = *reinterpret_cast<const unsigned short*>(blk + fp4_code<D>(t, c, v));
+    const unsigned hi = *reinterpret_cast<const unsigned short*>(blk + fp4_code<D>(t, c + 4, v));
+    return lo | (hi << 16);
+  }
+}
+template <int D>
+__device__ __forceinline__ void store_codes(unsigned char* blk, int t, int c, bool v, unsigned w) {
+  if constexpr (D == 128) {
+    *reinterpret_cast<unsigned*>(blk + fp4_code<D>(t, c, v)) = w;
+  } else {
+    *reinterpret_cast<unsigned short*>(blk + fp4_code<D>(t, c, v)) = (unsigned short)w;
+    *reinterpret_cast<unsigned short*>(blk + fp4_code<D>(t, c + 4, v)) = (unsigned short)(w >> 16);
+  }
+}
+
+// Eight channels of a token's K or V as four pairs of bf16, rounded: their codes, and the scale byte of the block
+// of 32 channels, which four neighbouring lanes hold (all four call this together).
+__device__ __forceinline__ void fp4_round(const unsigned (&w)[4], unsigned* code, unsigned* scale) {
+  // bf16 magnitudes order like the integers they are.
+  unsigned top = 0;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) top = max(top, max(w[k] & 0x7fffu, (w[k] >> 16) & 0x7fffu));
+  top = max(top, (unsigned)__shfl_xor((int)top, 1));
+  top = max(top, (unsigned)__shfl_xor((int)top, 2));
+  // Exponent of a, plus one from mantissa 0.75 on; two below it is the scale.
+  const unsigned byte = (unsigned)min(max((int)((top + 0x20u) >> 7) - 2, 2), 252);
+  const float s = __builtin_bit_cast(float, byte << 23);
+  unsigned q = 0;
+  q = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(q, __builtin_bit_cast(bf16x2_t, w[0]), s, 0);
+  q = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(q, __builtin_bit_cast(bf16x2_t, w[1]), s, 1);
+  q = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(q, __builtin_bit_cast(bf16x2_t, w[2]), s, 2);
+  q = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(q, __builtin_bit_cast(bf16x2_t, w[3]), s, 3);
+  const bool nan = top >= 0x7f80u;
+  *code = nan ? 0 : q;
+  *scale = nan ? 255 : byte;
+}
 
 }  // namespace
 }  // namespace ga

@@ -1,0 +1,103 @@
+// Kernel arguments of the calls between two attention calls (include/graphattn_step.h), and how their
+// kernels read a graph that lies in device memory: every index is checked where it is used.
+#pragma once
+
+#include "../../include/graphattn_step.h"
+#include "ga_internal.hpp"
+
+namespace ga {
+
+struct PageTableArgs {
+  const int32_t* seg_len;
+  const int64_t* old_offsets;
+  const int32_t* old_pages;
+  const int32_t* free_pages;
+  int64_t* offsets;
+  int32_t* pages;
+  int64_t n_old_pages, n_free, capacity;
+  int32_t S, S_old, spare;
+  int32_t tile;                  // segments of a workgroup (blockIdx.x), whose pages gridDim.y of them share
+};
+
+struct SlotMapArgs {
+  ga_device_graph g;
+  const int32_t* counts;
+  int32_t* offsets;
+  int32_t* words;
+  int32_t* positions;
+  int32_t* branches;
+  int32_t capacity;
+  int32_t tile;                  // branches of a workgroup, as above
+};
+
+struct QkvArgs {
+  const unsigned char* src[3];   // q, k, v
+  int64_t stride[3];             // bytes of a token
+  const int32_t* positions;
+  const int32_t* words;
+  unsigned char* q_out;
+  unsigned char* pool;
+  const double* inv_freq;
+  const float* weight[2];        // of q, of k; NULL: no norm
+  int64_t num_slots;
+  float eps, scale;
+  int32_t n, Hq, Hkv, half;      // half: rotary_dim / 2
+  int32_t per, parts;            // groups of heads of a wave, waves of a token
+};
+
+struct LogitArgs {
+  ga_device_graph g;
+  ga_logit_rules rules;
+  const unsigned char* in;
+  unsigned char* out;
+  int64_t in_stride, out_stride; // values
+  const int32_t* token_ids;
+  const int32_t* row_branches;
+  const int32_t* row_positions;
+  int32_t rows, vocab;
+  int32_t slice, parts;          // tokens of a workgroup (a multiple of 32), workgroups of a row
+  int32_t rows_per_xcd;
+  bool counted;                  // repetition, frequency or presence
+};
+
+hipError_t launch_page_table(const PageTableArgs& a, hipStream_t stream);
+hipError_t launch_slot_map(const SlotMapArgs& a, hipStream_t stream);
+hipError_t launch_qkv(const QkvArgs& a, int dim, int dtype, bool interleaved, hipStream_t stream);
+hipError_t launch_logits(const LogitArgs& a, bool in_f32, bool out_f32, hipStream_t stream);
+
+namespace {
+
+// A segment's pages in the table, and its tokens: empty for an id outside the graph.
+struct SegRange {
+  int64_t first, end;            // entries of seg_pages
+  int32_t len;
+};
+__device__ __forceinline__ SegRange seg_range(const ga_device_graph& g, int32_t s) {
+  if (s < 0 || s >= g.num_segments) return {0, 0, 0};
+  const int32_t len = g.seg_len[s];
+  const int64_t b = g.seg_page_offsets[s], e = g.seg_page_offsets[s + 1];
+  const bool in = b >= 0 && b <= g.num_table_pages;
+  return {in ? b : 0, in ? (e < g.num_table_pages ? e : g.num_table_pages) : 0, len > 0 ? len : 0};
+}
+
+// The page that holds token t of a segment, -1 where the table has none.
+__device__ __forceinline__ int32_t page_of(const ga_device_graph& g, int64_t first, int64_t end, int32_t t) {
+  const int64_t at = first + (t >> 4);
+  if (at >= end) return -1;
+  const int32_t page = g.seg_pages[at];
+  return page >= 0 && (int64_t)page < g.num_pages ? page : -1;
+}
+
+// Branch b's entries of path_segs.
+struct PathRange {
+  int64_t first, end;
+};
+__device__ __forceinline__ PathRange path_range(const ga_device_graph& g, int32_t b) {
+  const int64_t first = g.path_offsets[b], e = g.path_offsets[b + 1];
+  if (first < 0) return {0, 0};
+  return {first, e < g.num_path_segs ? e : g.num_path_segs};
+}
+
+}  // namespace
+
+}  // namespace ga

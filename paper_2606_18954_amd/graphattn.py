@@ -73,6 +73,31 @@ class Advantages(ctypes.Structure):
                 ("a_cor", ctypes.c_void_p), ("a_eff", ctypes.c_void_p), ("a_dual", ctypes.c_void_p)]
 
 
+class DeviceGraphC(ctypes.Structure):
+    _fields_ = [("num_segments", ctypes.c_int32), ("num_branches", ctypes.c_int32),
+                ("num_table_pages", ctypes.c_int64), ("num_path_segs", ctypes.c_int64),
+                ("num_pages", ctypes.c_int64), ("seg_len", ctypes.c_void_p),
+                ("seg_page_offsets", ctypes.c_void_p), ("seg_pages", ctypes.c_void_p),
+                ("path_offsets", ctypes.c_void_p), ("path_segs", ctypes.c_void_p)]
+
+
+class QKTransformC(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("norm_eps", ctypes.c_float), ("rotary_scale", ctypes.c_float),
+                ("inv_freq", ctypes.c_void_p), ("q_weight", ctypes.c_void_p),
+                ("k_weight", ctypes.c_void_p)]
+
+
+class LogitRulesC(ctypes.Structure):
+    _fields_ = [("repetition", ctypes.c_void_p), ("frequency", ctypes.c_void_p),
+                ("presence", ctypes.c_void_p), ("temperature", ctypes.c_void_p),
+                ("prompt_segments", ctypes.c_int32), ("bias_offsets", ctypes.c_void_p),
+                ("bias_tokens", ctypes.c_void_p), ("bias_values", ctypes.c_void_p),
+                ("num_bias", ctypes.c_int64), ("masks", ctypes.c_void_p),
+                ("num_masks", ctypes.c_int32), ("mask_words", ctypes.c_int64),
+                ("row_mask", ctypes.c_void_p)]
+
+
 class Profile(ctypes.Structure):
     _fields_ = [("schedules", ctypes.c_int32), ("runs", ctypes.c_int32),
                 ("sched_ms", ctypes.c_double), ("attn_ms", ctypes.c_double),
@@ -113,6 +138,16 @@ def load_library() -> ctypes.CDLL:
     lib.graphattn_kv_read.restype = ctypes.c_int
     lib.graphattn_kv_page_bytes.argtypes = [P(Params)]
     lib.graphattn_kv_page_bytes.restype = i64
+    lib.graphattn_page_table.argtypes = [vp, i32, i32, vp, vp, i32, i64, vp, i64, vp, vp, i64, vp]
+    lib.graphattn_page_table.restype = ctypes.c_int
+    lib.graphattn_slot_map.argtypes = [P(DeviceGraphC), vp, vp, vp, vp, vp, i32, vp]
+    lib.graphattn_slot_map.restype = ctypes.c_int
+    lib.graphattn_qkv_append.argtypes = [vp, vp, vp, vp, i64, i64, i64, vp, vp, i32, vp,
+                                         P(QKTransformC), P(Params), vp]
+    lib.graphattn_qkv_append.restype = ctypes.c_int
+    lib.graphattn_process_logits.argtypes = [vp, i64, i32, i32, i32, P(LogitRulesC), P(DeviceGraphC),
+                                             vp, vp, vp, vp, i64, i32, vp]
+    lib.graphattn_process_logits.restype = ctypes.c_int
     lib.graphattn_equivalence_classes.argtypes = [vp, i32, i32, P(StateForest), ctypes.c_float,
                                                   vp, vp]
     lib.graphattn_equivalence_classes.restype = ctypes.c_int
@@ -428,6 +463,237 @@ def empty_pool(params: Params, device="cuda"):
         return torch.empty((n, h, 17 * d), dtype=torch.uint8, device=device)
     dt = torch.float32 if params.dtype == GA_F32 else torch.bfloat16
     return torch.empty((n, h, 2, 16, d), dtype=dt, device=device)
+
+
+def _array(t, dtype, n: int, what: str) -> int:
+    """Pointer of a contiguous device tensor of this type with n elements at least (0 for None); `what` says so."""
+    if t is None:
+        return 0
+    if t.dtype != dtype or t.numel() < n or not t.is_contiguous():
+        raise ValueError(what)
+    if not t.is_cuda:
+        raise ValueError("tensors passed to the library must live on the GPU")
+    return t.data_ptr()
+
+
+class DeviceGraph:
+    """ga_device_graph: a rollout graph's index arrays as torch tensors on the device (kept, not copied: what a
+    call reads is what they hold when it runs).  seg_len int32 [S], seg_page_offsets int64 [S + 1], seg_pages
+    int32, path_offsets int64 [B + 1], path_segs int32; num_pages: of the pool."""
+
+    def __init__(self, seg_len, seg_page_offsets, seg_pages, path_offsets, path_segs, num_pages: int):
+        torch = _torch or _load_torch()
+        self.tensors = (seg_len, seg_page_offsets, seg_pages, path_offsets, path_segs)
+        self.num_segments, self.num_branches = int(seg_len.numel()), int(path_offsets.numel()) - 1
+        self.num_pages = int(num_pages)
+        if self.num_branches < 0:
+            raise ValueError("path_offsets must be int64 [branches + 1]")
+        S = self.num_segments
+        self.c = DeviceGraphC(
+            S, self.num_branches, int(seg_pages.numel()), int(path_segs.numel()), self.num_pages,
+            _array(seg_len, torch.int32, S, "seg_len must be int32, contiguous"),
+            _array(seg_page_offsets, torch.int64, S + 1, "seg_page_offsets must be int64 [segments + 1], contiguous"),
+            _array(seg_pages, torch.int32, 0, "seg_pages must be int32, contiguous"),
+            _array(path_offsets, torch.int64, 1, "path_offsets must be int64 [branches + 1], contiguous"),
+            _array(path_segs, torch.int32, 0, "path_segs must be int32, contiguous"))
+        self.ref = ctypes.byref(self.c)
+
+    @classmethod
+    def from_graph(cls, g: HostGraph, num_pages: int, device="cuda") -> "DeviceGraph":
+        """A copy of a host graph's arrays on the device."""
+        torch = _torch or _load_torch()
+        return cls(*(torch.from_numpy(a).to(device) for a in (g.seg_len, g.seg_page_offsets, g.seg_pages,
+                                                              g.path_offsets, g.path_segs)), num_pages)
+
+
+def page_table(seg_len, free_pages, spare: int = 0, old_offsets=None, old_pages=None, offsets=None, pages=None,
+               stream=None):
+    """graphattn_page_table: (seg_page_offsets int64 [S + 1], seg_pages int32) on the device.  Every segment keeps its
+    pages of the old table (its first len(old_offsets) - 1 segments) and gets more from the front of free_pages, for
+    seg_len + spare tokens.  Without `pages` a tensor of all old and free pages' size is made, -1 behind the table."""
+    torch = _torch or _load_torch()
+    lib = load_library()
+    S, known = int(seg_len.numel()), 0 if old_offsets is None else int(old_offsets.numel()) - 1
+    had = 0 if old_pages is None else int(old_pages.numel())
+    if known < 0 or (known > 0) > (old_pages is not None):
+        raise ValueError("old_offsets [segments + 1] and old_pages come together")
+    handle = _stream_handle(stream, seg_len) if seg_len.is_cuda else 0
+    if offsets is None:
+        offsets = torch.empty(S + 1, dtype=torch.int64, device=seg_len.device)
+    if pages is None:
+        pages = torch.full((had + int(free_pages.numel()),), -1, dtype=torch.int32, device=seg_len.device)
+    _check(lib.graphattn_page_table(
+        _array(seg_len, torch.int32, S, "seg_len must be int32, contiguous"), S, int(spare),
+        _array(old_offsets, torch.int64, 0, "old_offsets must be int64, contiguous"),
+        _array(old_pages, torch.int32, 0, "old_pages must be int32, contiguous"), known, had,
+        _array(free_pages, torch.int32, 0, "free_pages must be int32, contiguous"), int(free_pages.numel()),
+        _array(offsets, torch.int64, S + 1, "offsets must be int64 [segments + 1], contiguous"),
+        _array(pages, torch.int32, 0, "pages must be int32, contiguous"), int(pages.numel()), handle))
+    return offsets, pages
+
+
+def slot_map(graph: DeviceGraph, counts=None, token_offsets=None, slot_words=None, positions=None, branches=None,
+             capacity=None, stream=None):
+    """graphattn_slot_map: (token_offsets int32 [B + 1], slot_words, positions, branches int32 [capacity]) of every
+    branch's newest counts[b] tokens (one each without counts).  Where an output is given, it has the capacity; else
+    `capacity` (one row a branch without it)."""
+    torch = _torch or _load_torch()
+    lib = load_library()
+    B, given = graph.num_branches, [t for t in (slot_words, positions, branches) if t is not None]
+    device = graph.tensors[0].device
+    handle = _stream_handle(stream, graph.tensors[0])
+    n = min(int(t.numel()) for t in given) if given else B if capacity is None else int(capacity)
+    if capacity is not None and n < capacity:
+        raise ValueError("slot_words, positions and branches must be int32 [capacity], contiguous")
+    if not given:
+        slot_words, positions, branches = (torch.empty(n, dtype=torch.int32, device=device) for _ in range(3))
+    if token_offsets is None:
+        token_offsets = torch.empty(B + 1, dtype=torch.int32, device=device)
+    what = "slot_words, positions and branches must be int32 [capacity], contiguous"
+    _check(lib.graphattn_slot_map(
+        graph.ref, _array(counts, torch.int32, B, "counts must be int32 [branches], contiguous"),
+        _array(token_offsets, torch.int32, B + 1, "token_offsets must be int32 [branches + 1], contiguous"),
+        _array(slot_words, torch.int32, n, what), _array(positions, torch.int32, n, what),
+        _array(branches, torch.int32, n, what), n, handle))
+    return token_offsets, slot_words, positions, branches
+
+
+class QKTransform:
+    """ga_qk_transform: the norm of each head (q_norm, k_norm float32 [D], None: no norm) and the rotation by the
+    position (inv_freq float64 [rotary_dim / 2], radians a position; empty or None: none).  Channels i and i +
+    rotary_dim / 2 turn together, or 2i and 2i + 1 where interleaved; scale multiplies what turns."""
+
+    def __init__(self, head_dim: int, inv_freq=None, interleaved: bool = False, q_norm=None, k_norm=None,
+                 eps: float = 1e-6, scale: float = 1.0):
+        torch = _torch or _load_torch()
+        rotary = 0 if inv_freq is None else 2 * int(inv_freq.numel())
+        if rotary > head_dim:
+            raise ValueError(f"{rotary} rotated channels of {head_dim}")
+        if not scale:
+            raise ValueError("scale must not be 0")
+        self.head_dim, self.tensors = int(head_dim), (inv_freq, q_norm, k_norm)
+        what = "q_norm and k_norm must be float32 [head_dim], contiguous"
+        self.c = QKTransformC(rotary, int(bool(interleaved)), float(eps), float(scale),
+                              _array(inv_freq, torch.float64, 0, "inv_freq must be float64, contiguous"),
+                              _array(q_norm, torch.float32, head_dim, what),
+                              _array(k_norm, torch.float32, head_dim, what))
+        self.ref = ctypes.byref(self.c)
+
+
+def _rows(t, n: int, heads: int, dim: int, dtype) -> tuple:
+    """(pointer, values from a token's heads to the next one's) of rows [n, heads, dim]; the heads of a token lie one
+    behind the other."""
+    if t.dtype != dtype or tuple(t.shape) != (n, heads, dim):
+        raise ValueError(f"q, K and V rows beside this pool are {dtype} [tokens, heads, {dim}]")
+    token, head, channel = t.stride()
+    if n and (channel != 1 or (heads > 1 and head != dim)):
+        raise ValueError("the heads of a token must lie one behind the other")
+    if not t.is_cuda:
+        raise ValueError("tensors passed to the library must live on the GPU")
+    return t.data_ptr(), token if n > 1 else heads * dim
+
+
+def qkv_append(pool, q, k, v, positions, slot_words, transform: QKTransform, params: Params, q_out=None,
+               stream=None):
+    """graphattn_qkv_append: q [n, Hq, D] normed and rotated into q_out (returned), k [n, Hkv, D] likewise and v into the
+    pool's slots.  q, k and v may be parts of one projection's rows (strided tokens); positions and slot_words int32
+    [n]: a position below 0 is padding, a word outside the pool stores nothing."""
+    torch = _torch or _load_torch()
+    lib = load_library()
+    n, Hq, Hkv, D = int(positions.numel()), params.num_q_heads, params.num_kv_heads, params.head_dim
+    layout = _layout(params, n)
+    handle = _enter(stream, pool, layout)
+    row = layout[2] if layout else q.dtype
+    if transform.head_dim != D:
+        raise ValueError(f"a transform of {transform.head_dim}-wide heads for {D}-wide ones")
+    if q_out is None:
+        q_out = torch.zeros((n, Hq, D), dtype=row, device=q.device)
+    what = "positions and slot_words must be int32, one per token"
+    pw, ww = _array(positions, torch.int32, n, what), _array(slot_words, torch.int32, n, what)
+    (qp, qs), (kp, ks), (vp, vs) = (_rows(t, n, h, D, row) for t, h in ((q, Hq), (k, Hkv), (v, Hkv)))
+    op = _array(q_out, row, n * Hq * D, "q_out must be [tokens, Hq, D] of q's type, contiguous")
+    _check(lib.graphattn_qkv_append(_dev_ptr(pool), qp, kp, vp, qs, ks, vs, pw, ww, n, op, transform.ref,
+                                    ctypes.byref(params), handle))
+    return q_out
+
+
+class LogitRules:
+    """ga_logit_rules: per-row penalties and temperature (float32 [rows]), biases (CSR: bias_offsets int64 [rows + 1],
+    bias_tokens int32 ascending within a row, bias_values float32), grammar masks (int32 or uint32 [masks, words], a
+    set bit: the token may come) with row_mask int32 [rows] (outside [0, masks): none).  None leaves a rule out; the
+    first prompt_segments of a path count for the repetition penalty alone."""
+
+    def __init__(self, repetition=None, frequency=None, presence=None, temperature=None, prompt_segments: int = 0,
+                 bias_offsets=None, bias_tokens=None, bias_values=None, masks=None, row_mask=None):
+        torch = _torch or _load_torch()
+        self.tensors = (repetition, frequency, presence, temperature, bias_offsets, bias_tokens, bias_values, masks,
+                        row_mask)
+        per_row = [t for t in self.tensors[:4] + (row_mask,) if t is not None]
+        self.rows = min((int(t.numel()) for t in per_row), default=None)
+        biases = [t is not None for t in self.tensors[4:7]]
+        if any(biases) != all(biases):
+            raise ValueError("bias_offsets, bias_tokens and bias_values come together")
+        if (masks is None) != (row_mask is None):
+            raise ValueError("masks and row_mask come together")
+        nb = 0
+        if bias_tokens is not None:
+            nb = int(bias_tokens.numel())
+            at = int(bias_offsets.numel()) - 1
+            self.rows = at if self.rows is None else min(self.rows, at)
+        self.vocab, (nm, words) = None, (0, 0)
+        if masks is not None:
+            if masks.dim() != 2 or masks.element_size() != 4 or masks.is_floating_point():
+                raise ValueError("masks must be int32 or uint32 [masks, words]")
+            nm, words = masks.shape
+            self.vocab = 32 * words
+        self.counted = any(t is not None for t in self.tensors[:3])
+        what = "penalties and temperature must be float32 [rows], contiguous"
+        self.c = LogitRulesC(
+            *(_array(t, torch.float32, 0, what) for t in self.tensors[:4]), int(prompt_segments),
+            _array(bias_offsets, torch.int64, 1, "bias_offsets must be int64 [rows + 1], contiguous"),
+            _array(bias_tokens, torch.int32, 0, "bias_tokens must be int32, contiguous"),
+            _array(bias_values, torch.float32, nb, "bias_values must be float32, one per token, contiguous"), nb,
+            0 if masks is None else _array(masks, masks.dtype, 0, "masks must be contiguous"), nm, words,
+            _array(row_mask, torch.int32, 0, "row_mask must be int32 [rows], contiguous"))
+        self.ref = ctypes.byref(self.c)
+
+
+def process_logits(logits, rules: LogitRules, graph: Optional[DeviceGraph] = None, token_ids=None, row_branches=None,
+                   row_positions=None, out=None, out_f32: bool = False, stream=None):
+    """graphattn_process_logits: logits [rows, vocab] (float32 or bfloat16; rows may be strided) through the rules,
+    into out (returned; `logits` itself: in place).  token_ids int32 [num_pages x 16]: the token of every slot;
+    row_branches and row_positions int32 [rows] as slot_map writes them (None: row r is branch r and sees its whole
+    path).  Rows of padding are left as they were (zero where this call allocates)."""
+    torch = _torch or _load_torch()
+    lib = load_library()
+    if logits.dim() != 2 or logits.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("logits must be float32 or bfloat16 [rows, vocab]")
+    rows, vocab = logits.shape
+    handle = _stream_handle(stream, logits) if logits.is_cuda else 0
+    if out is None:
+        out = torch.zeros((rows, vocab), dtype=torch.float32 if out_f32 else logits.dtype, device=logits.device)
+    if out.shape != logits.shape or out.dtype not in (torch.float32, logits.dtype):
+        raise ValueError("out must be [rows, vocab], float32 or of the logits' type")
+    if rules.rows is not None and rules.rows < rows:
+        raise ValueError("the rules have fewer rows than the logits")
+    if rules.vocab is not None and rules.vocab < vocab:
+        raise ValueError("the masks have fewer tokens than the logits")
+    if rules.counted and (graph is None or token_ids is None):
+        raise ValueError("penalties need the graph and its slots' token_ids")
+    if rows and vocab and (logits.stride(1) != 1 or out.stride(1) != 1):
+        raise ValueError("the values of a row must lie one behind the other")
+    what = "row_branches and row_positions must be int32 [rows], contiguous"
+    ids = _array(token_ids, torch.int32, 16 * graph.num_pages if graph is not None else 0,
+                 "token_ids must be int32, one per slot of the pool, contiguous")
+    bw, pw = _array(row_branches, torch.int32, rows, what), _array(row_positions, torch.int32, rows, what)
+    if not (logits.is_cuda and out.is_cuda):
+        raise ValueError("tensors passed to the library must live on the GPU")
+    si, so = (t.stride(0) if rows > 1 else vocab for t in (logits, out))
+    _check(lib.graphattn_process_logits(
+        logits.data_ptr(), si, rows, vocab, GA_F32 if logits.dtype == torch.float32 else GA_BF16, rules.ref,
+        graph.ref if graph is not None else None, ids, bw, pw, out.data_ptr(), so,
+        int(out.dtype == torch.float32), handle))
+    return out
 
 
 class HostForest:
