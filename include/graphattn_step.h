@@ -112,7 +112,7 @@ typedef struct {
   const float* repetition;     /* [rows] r: a token of the context has its logit z become z / r where z > 0, else z r */
   const float* frequency;      /* [rows] f: f times its count in the context, the prompt aside, is taken off */
   const float* presence;       /* [rows] taken off once where that count is not 0 */
-  const float* temperature;    /* [rows] z / temperature (as z times its float32 reciprocal) */
+  const float* temperature;    /* [rows] z / temperature (this and z / r: as z times the float32 reciprocal) */
   int32_t prompt_segments;     /* the first so many segments of every path are the prompt (>= 0) */
   const int64_t* bias_offsets; /* [rows + 1] CSR into bias_tokens and bias_values; entries outside [0, num_bias)
                                   are left out */
@@ -142,7 +142,8 @@ typedef struct {
  *   token_ids     [num_pages x 16] device int32, one per slot of the pool
  * Where neither repetition, frequency nor presence is given the context is not read, and graph and token_ids may
  * be NULL (row_branches and row_positions mark padding all the same).  A mask that forbids everything leaves a row
- * of -infinity.  A token's count is exact up to 2^30 - 1. */
+ * of -infinity.  Of a context the first 2^31 - 1 tokens
+ * are seen, and a token's count is exact up to 2^30 - 1. */
 ga_status graphattn_process_logits(const void* logits, int64_t logits_stride, int32_t rows,
                                    int32_t vocab, int32_t dtype, const ga_logit_rules* rules,
                                    const ga_device_graph* graph, const int32_t* token_ids,

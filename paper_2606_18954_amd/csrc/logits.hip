@@ -11,6 +11,8 @@
 // from L2: rows of one XCD are neighbours, whose paths share segments).
 // Biases: the flag says that there is one, and its value is looked up (the row's list is ascending).
 // Memory bounds it: a row of V values of four bytes moves 8 V.
+#include <type_traits>
+
 #include "pool_load.hpp"
 #include "step_internal.hpp"
 
@@ -19,84 +21,128 @@ namespace {
 
 constexpr int kThreads = 512;
 constexpr int kPath = 64;          // segments of a path taken at once
-constexpr int kAhead = 4;          // tokens of a thread whose loads are in flight together
-constexpr int kMaxSlice = 19456;   // 2 bytes a token: 38 KB, four workgroups a CU
+constexpr int kAhead = 2;          // fours of tokens of a thread whose loads are in flight together
+constexpr int kBias = 512;         // biases of a row that LDS holds; a longer list is looked up in memory
+// Tokens of a slice, so that four workgroups share a CU's LDS: 38 KB of counts, or 34 and the biases.
+constexpr int kMaxSlice = 19456, kMaxSliceBiased = 17408;
 
 typedef unsigned u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef int i32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 
 struct Path {
   int64_t first[kPath], last[kPath];     // pages of the segments
-  int64_t end[kPath];                    // tokens of the path up to and with each (of these kPath)
+  int32_t end[kPath];                    // fours of tokens up to and with each (of these kPath)
+  int32_t tokens[kPath];                 // that the row sees
   bool prompt[kPath];
 };
 
-// What a wave found in them: tokens, and how many of them before a position are not the prompt's.
+// What a wave found in them: tokens, fours of tokens that the row sees, and such tokens that are not the prompt's.
 struct Found {
   int64_t tokens, said;
+  int32_t fours;
 };
 
-template <class TI, class TO>
 struct Row {
   const unsigned char* in;
   unsigned char* out;
-  float rep, freq, pres, inv_t;
+  float rep, inv_rep, freq, pres, inv_t;
   const uint32_t* mask;                  // or NULL
-  int64_t bias_first, bias_end;
 };
 
-__device__ __forceinline__ int64_t wave_sum(int64_t v) {
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d);
-  return v;
+// The last lane's value, in every lane.
+__device__ __forceinline__ int64_t last_lane(int64_t v) {
+  const unsigned lo = (unsigned)__builtin_amdgcn_readlane((int)v, 63);
+  const int hi = __builtin_amdgcn_readlane((int)(v >> 32), 63);
+  return (int64_t)(((uint64_t)(unsigned)hi << 32) | lo);
 }
 
-// Entries [at, at + kPath) of a path, by one wave; `start` is the position of their first token.  Entries behind the
-// path's last are empty.
+// Entries [at, at + kPath) of a path, by one wave; `start` is the position of their first token, and positions from
+// `limit` on are not seen.  Entries behind the path's last are empty.
 __device__ __forceinline__ Found take_path(const LogitArgs& a, const PathRange& range, int64_t at, int64_t start,
                                            int64_t limit, Path* p) {
   const int lane = threadIdx.x & 63;
   const int64_t e = range.first + at + lane;
-  const int n = (int)(range.end - range.first - at < kPath ? range.end - range.first - at : kPath);
-  const SegRange s = lane < n ? seg_range(a.g, a.g.path_segs[e]) : SegRange{0, 0, 0};
-  int64_t end = s.len;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int64_t x = __shfl_up(end, d);
-    if (lane >= d) end += x;
-  }
+  const SegRange s = e < range.end ? seg_range(a.g, a.g.path_segs[e]) : SegRange{0, 0, 0};
+  const int64_t end = wave_scan(s.len);
+  const int64_t room = limit - (start + end - s.len);
+  const int32_t seen = room <= 0 ? 0 : s.len < room ? s.len : (int32_t)room;
+  const int64_t fours = wave_scan((seen + 3LL) / 4);
   const bool prompt = at + lane < a.rules.prompt_segments;
   p->first[lane] = s.first;
   p->last[lane] = s.end;
-  p->end[lane] = end;
+  p->end[lane] = (int32_t)fours;
+  p->tokens[lane] = seen;
   p->prompt[lane] = prompt;
-  const int64_t room = limit - (start + end - s.len);
-  return {__shfl(end, 63), wave_sum(prompt || room <= 0 ? 0 : s.len < room ? s.len : room)};
+  return {last_lane(end), last_lane(wave_scan(prompt ? 0 : seen)), __builtin_amdgcn_readlane((int)fours, 63)};
 }
 
-template <class TI, class TO>
-__device__ __forceinline__ float bias_of(const LogitArgs& a, const Row<TI, TO>& row, int v) {
-  int64_t lo = row.bias_first, hi = row.bias_end;
+// The sum of a token's values in a list that is ascending by token.
+__device__ __forceinline__ float sum_of(const int32_t* tokens, const float* values, int n, int v) {
+  int lo = 0, hi = n;
   while (lo < hi) {
-    const int64_t mid = lo + (hi - lo) / 2;
-    if (a.rules.bias_tokens[mid] < v) lo = mid + 1;
+    const int mid = lo + (hi - lo) / 2;
+    if (tokens[mid] < v) lo = mid + 1;
     else hi = mid;
   }
   float s = 0.f;
-  for (; lo < row.bias_end && a.rules.bias_tokens[lo] == v; ++lo) s += a.rules.bias_values[lo];
+  for (; lo < n && tokens[lo] == v; ++lo) s += values[lo];
   return s;
 }
 
-template <class TO>
-__device__ __forceinline__ void put(unsigned char* out, int64_t v, float z) {
-  reinterpret_cast<TO*>(out)[v] = (TO)z;
+// Values as they are loaded: as many as are 16 bytes of the wider type.
+template <class T, int E>
+struct Values {
+  static constexpr int W = E * sizeof(T) / 4;
+  unsigned w[W];
+  __device__ __forceinline__ void load(const unsigned char* row, int v) {
+    typedef unsigned words __attribute__((ext_vector_type(W), aligned(2)));
+    const words x = __builtin_nontemporal_load(reinterpret_cast<const words*>(row + (unsigned)v * (unsigned)sizeof(T)));
+#pragma unroll
+    for (int k = 0; k < W; ++k) w[k] = x[k];
+  }
+  __device__ __forceinline__ void load_some(const unsigned char* row, int v, int n) {
+#pragma unroll
+    for (int k = 0; k < W; ++k) w[k] = 0;
+#pragma unroll
+    for (int k = 0; k < E; ++k)
+      if (k < n) {
+        const T x = reinterpret_cast<const T*>(row)[v + k];
+        if constexpr (sizeof(T) == 4) w[k] = __builtin_bit_cast(unsigned, x);
+        else w[k / 2] |= (unsigned)__builtin_bit_cast(unsigned short, x) << (16 * (k & 1));
+      }
+  }
+  __device__ __forceinline__ float at(int k) const {
+    const unsigned u = sizeof(T) == 4 ? w[k] : k & 1 ? w[k / 2] & 0xffff0000u : w[k / 2] << 16;
+    return __builtin_bit_cast(float, u);
+  }
+};
+
+template <class TO, int E>
+__device__ __forceinline__ void store(unsigned char* row, int v, const float (&z)[E]) {
+  unsigned char* const to = row + (unsigned)v * (unsigned)sizeof(TO);
+#pragma unroll
+  for (int i = 0; i < E * (int)sizeof(TO) / 16; ++i) {
+    u32x4 w;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if constexpr (sizeof(TO) == 4) {
+        w[k] = __builtin_bit_cast(unsigned, z[4 * i + k]);
+      } else {
+        typedef __bf16 two __attribute__((ext_vector_type(2)));
+        w[k] = __builtin_bit_cast(unsigned, two{(__bf16)z[2 * k], (__bf16)z[2 * k + 1]});
+      }
+    }
+    reinterpret_cast<u32x4_any*>(to)[i] = w;
+  }
 }
 
 template <class TI, class TO>
-__global__ __launch_bounds__(kThreads) void k_logits(LogitArgs a) {
-  constexpr int E = 16 / sizeof(TI);                 // values of a load
+__global__ __launch_bounds__(kThreads, 8) void k_logits(LogitArgs a) {
+  constexpr int E = 16 / sizeof(TO), LOADS = sizeof(TI) == 4 ? 3 : 16 / E;  // values of a load; loads of a thread in flight together
   extern __shared__ unsigned counts[];
   __shared__ Path path;
   __shared__ int64_t said_of, tokens_of;
+  __shared__ int32_t fours_of;
   const int tid = threadIdx.x;
   // Workgroups go round the 8 XCDs: a row's stay on one, with its neighbours'.
   const int64_t q = blockIdx.x / 8;
@@ -105,16 +151,26 @@ __global__ __launch_bounds__(kThreads) void k_logits(LogitArgs a) {
   const int lo0 = (int)(q % a.parts) * a.slice, hi0 = min(lo0 + a.slice, a.vocab);
   const int32_t b = a.row_branches ? a.row_branches[r] : (int32_t)r;
   if (b < 0 || b >= a.g.num_branches) return;
-  int64_t limit = 1LL << 62;
+  int64_t limit = 0x7fffffff;
   if (a.row_positions) {
     const int32_t p = a.row_positions[r];
     if (p < 0) return;
     limit = (int64_t)p + 1;
   }
-  Row<TI, TO> row;
+  Row row;
   row.in = a.in + r * a.in_stride * (int64_t)sizeof(TI);
   row.out = a.out + r * a.out_stride * (int64_t)sizeof(TO);
+  Values<TI, E> x[LOADS];
+  const auto fetch = [&](int v0, int hi) {
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int v = v0 + E * (tid + i * kThreads);
+      if (v + E <= hi) x[i].load(row.in, v);
+      else x[i].load_some(row.in, v, hi - v);
+    }
+  };
   row.rep = a.rules.repetition ? a.rules.repetition[r] : 1.f;
+  row.inv_rep = 1.f / row.rep;
   row.freq = a.rules.frequency ? a.rules.frequency[r] : 0.f;
   row.pres = a.rules.presence ? a.rules.presence[r] : 0.f;
   row.inv_t = a.rules.temperature ? 1.f / a.rules.temperature[r] : 1.f;
@@ -123,22 +179,30 @@ __global__ __launch_bounds__(kThreads) void k_logits(LogitArgs a) {
     const int32_t m = a.rules.row_mask[r];
     if (m >= 0 && m < a.rules.num_masks) row.mask = a.rules.masks + m * a.rules.mask_words;
   }
-  row.bias_first = row.bias_end = 0;
+  int64_t bias_first = 0, bias_end = 0;
   if (a.rules.bias_offsets) {
     const int64_t f = a.rules.bias_offsets[r], e = a.rules.bias_offsets[r + 1];
-    row.bias_first = f < 0 ? 0 : f;
-    row.bias_end = e < a.rules.num_bias ? e : a.rules.num_bias;
+    bias_first = f < 0 ? 0 : f;
+    bias_end = e < a.rules.num_bias ? e : a.rules.num_bias;
   }
-  const bool biased = row.bias_first < row.bias_end;
+  const bool biased = bias_first < bias_end;
 
+  // Values of the first loads, counts of 0, and, by one wave, the path: before they are waited for.
+  fetch(lo0, hi0);
+  const bool flags = a.counted || biased;
+  const auto clear = [&]() {
+    typedef unsigned u32x4_lds __attribute__((ext_vector_type(4), aligned(16)));
+    for (int i = tid; i < a.slice / 8 + 4; i += kThreads) reinterpret_cast<u32x4_lds*>(counts)[i] = u32x4_lds{0, 0, 0, 0};
+  };
+  if (flags) clear();
   PathRange range{0, 0};
   int64_t said = 0, chunks = 0;
   if (a.counted) {
     range = path_range(a.g, b);
-    chunks = range.end > range.first ? (range.end - range.first + kPath - 1) / kPath : 0;
+    chunks = (range.end - range.first + kPath - 1) / kPath;
     if (tid < 64) {
       int64_t start = 0;
-      Found f{0, 0};
+      Found f{0, 0, 0};
       for (int64_t c = 0; c < chunks; ++c) {
         f = take_path(a, range, c * kPath, start, limit, &path);
         said += f.said;
@@ -147,31 +211,34 @@ __global__ __launch_bounds__(kThreads) void k_logits(LogitArgs a) {
       if (tid == 0) {
         said_of = said;
         tokens_of = f.tokens;
+        fours_of = f.fours;
       }
     }
-    __syncthreads();
-    said = said_of;
   }
+  if (flags) __syncthreads();
+  if (a.counted) said = said_of;
   const bool wide = said > 0x3fff;
-  const bool flags = a.counted || biased;
+  const int n_bias = (int)min(bias_end - bias_first, (int64_t)0x7fffffff);
+  const bool near = biased && n_bias <= kBias;
+  int32_t* const near_tokens = reinterpret_cast<int32_t*>(counts + a.slice / 2 + 16);
+  float* const near_values = reinterpret_cast<float*>(near_tokens + kBias);
 
-  for (int half = 0; half < (wide ? 2 : 1); ++half) {
-    const int step = wide ? (a.slice / 2 + 31) / 32 * 32 : a.slice;
-    const int lo = lo0 + half * step, hi = half == 0 ? min(lo0 + step, hi0) : hi0;
-    if (lo >= hi) break;
-    if (flags) {
-      if (half) __syncthreads();
-      const int words = wide ? hi - lo : (hi - lo + 1) / 2;
-      for (int i = tid; i < words; i += kThreads) counts[i] = 0;
+  // The slice [lo, hi), with counts of 16 or 32 bits.
+  const auto pass = [&](auto wide_counts, int lo, int hi) {
+    constexpr bool WIDE = decltype(wide_counts)::value;
+    if (lo != lo0) {
+      fetch(lo, hi);
+      __syncthreads();
+      clear();
       __syncthreads();
     }
-    const auto note = [&](int v) {
-      if (wide) atomicAdd(&counts[v - lo], 1u);
-      else atomicAdd(&counts[(v - lo) >> 1], 1u << (((v - lo) & 1) * 16));
+    const auto note = [&](int v) {                   // (v: from lo on)
+      if constexpr (WIDE) atomicAdd(&counts[v], 1u);
+      else atomicAdd(&counts[v >> 1], 1u << ((v & 1) * 16));
     };
-    const auto flag = [&](int v, unsigned n) {       // (as 16 bits hold it)
-      if (wide) atomicOr(&counts[v - lo], n << 16);
-      else atomicOr(&counts[(v - lo) >> 1], n << (((v - lo) & 1) * 16));
+    const auto flag = [&](int v, unsigned n) {       // (n: as 16 bits hold it)
+      if constexpr (WIDE) atomicOr(&counts[v], n << 16);
+      else atomicOr(&counts[v >> 1], n << ((v & 1) * 16));
     };
     int64_t start = 0;
     for (int64_t c = 0; c < chunks; ++c) {
@@ -179,117 +246,126 @@ __global__ __launch_bounds__(kThreads) void k_logits(LogitArgs a) {
         __syncthreads();
         if (tid < 64) {
           const Found f = take_path(a, range, c * kPath, start, limit, &path);
-          if (tid == 0) tokens_of = f.tokens;
+          if (tid == 0) {
+            tokens_of = f.tokens;
+            fours_of = f.fours;
+          }
         }
         __syncthreads();
       }
-      const int64_t tokens = tokens_of, left = limit - start;
-      const int64_t n = tokens < left ? tokens : left;
-      for (int64_t i0 = tid; i0 < n; i0 += kAhead * kThreads) {
-        int32_t slot[kAhead];
+      // Four tokens a thread: a segment starts a page, so they lie in one.
+      const int n = fours_of;
+      for (int i0 = tid; i0 < n; i0 += kAhead * kThreads) {
+        int32_t slot[kAhead], left[kAhead];          // of the first token; tokens that are seen
         bool prompt[kAhead];
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
-          const int64_t i = i0 + k * kThreads;
+          const int i = i0 + k * kThreads;
           slot[k] = -1;
+          left[k] = 0;
           prompt[k] = false;
           if (i < n) {
             int s = 0;                               // the first segment that ends behind i
             for (int d = kPath / 2; d > 0; d >>= 1)
               if (path.end[s + d - 1] <= i) s += d;
-            const int32_t t = (int32_t)(i - (s ? path.end[s - 1] : 0));
+            const int32_t t = 4 * (i - (s ? path.end[s - 1] : 0));
             const int32_t page = page_of(a.g, path.first[s], path.last[s], t);
             slot[k] = page < 0 ? -1 : page * kPageTokens + (t & (kPageTokens - 1));
+            left[k] = page < 0 ? 0 : path.tokens[s] - t;
             prompt[k] = path.prompt[s];
           }
         }
-        int32_t id[kAhead];
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k) id[k] = slot[k] >= 0 ? a.token_ids[slot[k]] : -1;
+        i32x4_any id[kAhead];
 #pragma unroll
         for (int k = 0; k < kAhead; ++k)
-          if (id[k] >= lo && id[k] < hi) {
-            if (prompt[k]) flag(id[k], 0x8000u);
-            else note(id[k]);
+          if (slot[k] >= 0) id[k] = *reinterpret_cast<const i32x4_any*>(a.token_ids + slot[k]);
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int32_t v = id[k][e];
+            if (e < left[k] && v >= lo && v < hi) {
+              if (prompt[k]) flag(v - lo, 0x8000u);
+              else note(v - lo);
+            }
           }
       }
-      start += tokens;
+      start += tokens_of;
     }
     if (biased)
-      for (int64_t e = row.bias_first + tid; e < row.bias_end; e += kThreads) {
-        const int v = a.rules.bias_tokens[e];
-        if (v >= lo && v < hi) flag(v, 0x4000u);
+      for (unsigned e = tid; e < (unsigned)n_bias; e += kThreads) {
+        const int v = a.rules.bias_tokens[bias_first + e];
+        if (v >= lo && v < hi) flag(v - lo, 0x4000u);
+        if (near) {
+          near_tokens[e] = v;
+          near_values[e] = a.rules.bias_values[bias_first + e];
+        }
       }
     if (flags) __syncthreads();
 
-    const auto rule = [&](float z, unsigned word, int v) {   // word: as 32 bits hold it
-      const unsigned count = word & 0x3fffffffu;
-      if (word & 0x40000000u) z += bias_of(a, row, v);
-      if (word & 0xbfffffffu) z = z > 0.f ? z / row.rep : z * row.rep;
-      if (count) z -= row.freq * (float)count + row.pres;
-      return z;
-    };
-    const auto wide_word = [](unsigned w16) { return ((w16 & 0xc000u) << 16) | (w16 & 0x3fffu); };
-    for (int v0 = lo + E * tid; v0 < hi; v0 += E * kThreads) {
-      const int m = min(E, hi - v0);
-      float z[E];
-      if (m == E) {
-        const u32x4 w = *reinterpret_cast<const u32x4_any*>(row.in + (int64_t)v0 * sizeof(TI));
+    for (int v0 = lo; v0 < hi; v0 += E * LOADS * kThreads) {
+      if (v0 != lo) fetch(v0, hi);
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const int v = v0 + E * (tid + i * kThreads), m = min(E, hi - v);
+        if (m <= 0) continue;
+        unsigned allowed = ~0u;
+        if (row.mask) allowed = row.mask[v >> 5] >> (v & 31);
+        float z[E];
+#pragma unroll
+        for (int k = 0; k < E; ++k) z[k] = x[i].at(k);
+        if (flags) {
+          constexpr int W = WIDE ? E : E / 2;
+          const unsigned* const word = counts + (WIDE ? v - lo : (v - lo) >> 1);
+          unsigned w[W], any = 0;
+#pragma unroll
+          for (int k = 0; k < W; ++k) any |= w[k] = word[k];
+          // The tokens that have a bias, one after the other: few have.
+          if (any & (WIDE ? 0x40000000u : 0x40004000u)) {
+            unsigned some = 0;
+#pragma unroll
+            for (int k = 0; k < E; ++k)
+              some |= w[WIDE ? k : k / 2] & (WIDE ? 0x40000000u : k & 1 ? 0x40000000u : 0x4000u) ? 1u << k : 0u;
+            for (some &= (1u << m) - 1; some; some &= some - 1) {
+              const int j = __builtin_ctz(some);
+              const float bias =
+                  near ? sum_of(near_tokens, near_values, n_bias, v + j)
+                       : sum_of(a.rules.bias_tokens + bias_first, a.rules.bias_values + bias_first, n_bias, v + j);
+#pragma unroll
+              for (int k = 0; k < E; ++k) z[k] += j == k ? bias : 0.f;
+            }
+          }
+          if (any && a.counted)
+#pragma unroll
+            for (int k = 0; k < E; ++k) {
+              const unsigned u = WIDE ? w[k] : k & 1 ? w[k / 2] >> 16 : w[k / 2] & 0xffffu;
+              const unsigned count = u & (WIDE ? 0x3fffffffu : 0x3fffu);
+              const float size = z[k] > 0.f ? row.inv_rep : row.rep;
+              if (u & (WIDE ? 0xbfffffffu : 0xbfffu)) z[k] *= size;
+              if (count) z[k] -= row.freq * (float)count + row.pres;
+            }
+        }
 #pragma unroll
         for (int k = 0; k < E; ++k) {
-          // (a vector's element is no object that bit_cast could take)
-          const unsigned u = sizeof(TI) == 4 ? w[k] : k & 1 ? w[k / 2] & 0xffff0000u : w[k / 2] << 16;
-          z[k] = __builtin_bit_cast(float, u);
+          z[k] *= row.inv_t;
+          if (!((allowed >> k) & 1)) z[k] = -__builtin_inff();
         }
-      } else {
-#pragma unroll
-        for (int k = 0; k < E; ++k) z[k] = k < m ? (float)reinterpret_cast<const TI*>(row.in)[v0 + k] : 0.f;
-      }
-      unsigned allowed = ~0u;
-      if (row.mask) allowed = row.mask[v0 >> 5] >> (v0 & 31);
-      if (flags) {
-        const int at = v0 - lo;
-        unsigned w[E], any = 0;
-#pragma unroll
-        for (int k = 0; k < E; ++k) {
-          if (wide) w[k] = k < m ? counts[at + k] : 0;
-          else w[k] = k < m ? (counts[(at + k) >> 1] >> ((k & 1) * 16)) & 0xffffu : 0;
-          any |= w[k];
-        }
-        if (any)
+        if (m == E) {
+          store<TO, E>(row.out, v, z);
+        } else {
 #pragma unroll
           for (int k = 0; k < E; ++k)
-            if (w[k]) z[k] = rule(z[k], wide ? w[k] : wide_word(w[k]), v0 + k);
-      }
-#pragma unroll
-      for (int k = 0; k < E; ++k) {
-        z[k] *= row.inv_t;
-        if (!((allowed >> k) & 1)) z[k] = -__builtin_inff();
-      }
-      if (m == E) {
-        if constexpr (sizeof(TO) == 4) {
-#pragma unroll
-          for (int i = 0; i < E / 4; ++i) {
-            u32x4 w;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) w[k] = __builtin_bit_cast(unsigned, z[4 * i + k]);
-            reinterpret_cast<u32x4_any*>(row.out + (int64_t)v0 * 4)[i] = w;
-          }
-        } else {
-          u32x4 w;
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            typedef __bf16 two __attribute__((ext_vector_type(2)));
-            w[k] = __builtin_bit_cast(unsigned, two{(__bf16)z[2 * k], (__bf16)z[2 * k + 1]});
-          }
-          *reinterpret_cast<u32x4_any*>(row.out + (int64_t)v0 * 2) = w;
+            if (k < m) reinterpret_cast<TO*>(row.out)[v + k] = (TO)z[k];
         }
-      } else {
-#pragma unroll
-        for (int k = 0; k < E; ++k)
-          if (k < m) put<TO>(row.out, v0 + k, z[k]);
       }
     }
+  };
+  if (!wide) {
+    pass(std::false_type{}, lo0, hi0);
+  } else {
+    const int mid = min(lo0 + (a.slice / 2 + 31) / 32 * 32, hi0);
+    pass(std::true_type{}, lo0, mid);
+    if (mid < hi0) pass(std::true_type{}, mid, hi0);
   }
 }
 
@@ -298,7 +374,9 @@ __global__ __launch_bounds__(kThreads) void k_logits(LogitArgs a) {
 hipError_t launch_logits(const LogitArgs& args, bool in_f32, bool out_f32, hipStream_t stream) {
   LogitArgs a = args;
   // Slices of a row: as many as its counts need, and so many that a few rows fill the device.
-  const int64_t least = (a.vocab + kMaxSlice - 1) / kMaxSlice, most = (a.vocab + 2047) / 2048;
+  const bool biased = a.rules.bias_offsets != nullptr;
+  const int64_t largest = biased ? kMaxSliceBiased : kMaxSlice;
+  const int64_t least = (a.vocab + largest - 1) / largest, most = (a.vocab + 2047) / 2048;
   int64_t parts = (1024 + a.rows - 1) / a.rows;
   parts = parts < least ? least : parts > most ? most : parts;
   a.slice = (int32_t)(((a.vocab + parts - 1) / parts + 31) / 32 * 32);
@@ -306,7 +384,7 @@ hipError_t launch_logits(const LogitArgs& args, bool in_f32, bool out_f32, hipSt
   a.rows_per_xcd = (a.rows + 7) / 8;
   const int64_t grid = (int64_t)a.rows_per_xcd * 8 * a.parts;
   if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
-  const size_t lds = (size_t)a.slice * 2 + 64;
+  const size_t lds = (size_t)a.slice * 2 + 64 + (biased ? kBias * 8 : 0);
   const dim3 g((unsigned)grid), t(kThreads);
   if (in_f32) hipLaunchKernelGGL((k_logits<float, float>), g, t, lds, stream, a);
   else if (out_f32) hipLaunchKernelGGL((k_logits<__bf16, float>), g, t, lds, stream, a);

@@ -20,6 +20,12 @@ namespace {
 
 constexpr int kWaves = 4;          // of a workgroup
 
+// Groups of heads that a wave takes at once, all of their loads ahead of the first store: of q, or of k and of v.
+template <class T>
+struct Units {
+  static constexpr int Q = sizeof(T) == 4 ? 3 : 5, KV = sizeof(T) == 4 ? 1 : 2;
+};
+
 __device__ __forceinline__ float bf16_lo(unsigned w) { return __builtin_bit_cast(float, w << 16); }
 __device__ __forceinline__ float bf16_hi(unsigned w) { return __builtin_bit_cast(float, w & 0xffff0000u); }
 __device__ __forceinline__ unsigned bf16_pair(float lo, float hi) {
@@ -73,135 +79,179 @@ __device__ __forceinline__ float head_sum(float s) {
   return s;
 }
 
+// What the heads of a kind are made with: cosine and sine of this lane's channels (the sine with its sign), weights folded
+// in, and where the partners are.
+struct Turn {
+  float c[8], s[8];
+  bool normed;
+};
+
 template <int D, class T, bool FP4, bool PAIRS>
 __global__ __launch_bounds__(64 * kWaves) void k_qkv(QkvArgs a) {
-  constexpr int LPH = D / 8, HPG = 64 / LPH, ROW = D * (int)sizeof(T);
+  constexpr int LPH = D / 8, HPG = 64 / LPH, SZ = (int)sizeof(T), ROW = D * SZ;
+  using U = Units<T>;
+  __shared__ __align__(16) float cosines[kWaves][64], sines[kWaves][64], weights[2 * D];
   const int lane = threadIdx.x & 63;
-  const unsigned task = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * kWaves + (threadIdx.x >> 6)));
-  const unsigned token = task / (unsigned)a.parts;
-  if (token >= (unsigned)a.n) return;
-  const int32_t pos = a.positions[token];
-  if (pos < 0) return;
-  const int32_t word = a.words[token];
-  const bool stored = word >= 0 && (int64_t)word < a.num_slots;
-  const int g = lane / LPH, c = 8 * (lane % LPH);
-  const int nq = (a.Hq + HPG - 1) / HPG, nk = (a.Hkv + HPG - 1) / HPG;
-  int it = (int)(task - token * a.parts) * a.per;
-  const int end = min(it + a.per, stored ? nq + 2 * nk : nq);
-  if (it >= end) return;
-
-  auto kind_of = [&](int i) { return i < nq ? 0 : i < nq + nk ? 1 : 2; };
-  auto head_of = [&](int i, int kind) { return (i - (kind == 0 ? 0 : kind == 1 ? nq : nq + nk)) * HPG + g; };
-  auto fetch = [&](int i, Raw<T>* r) {
-    const int kind = kind_of(i), h = head_of(i, kind);
-    if (h < (kind == 0 ? a.Hq : a.Hkv))
-      r->load(a.src[kind] + (int64_t)token * a.stride[kind] + h * ROW + c * (int)sizeof(T));
-    else
-#pragma unroll
-      for (int k = 0; k < Raw<T>::W; ++k) r->w[k] = 0;
-  };
-  Raw<T> next;
-  fetch(it, &next);
-
-  // Sine and cosine of this lane's channels, the sine with its sign.
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const int64_t first = (int64_t)blockIdx.x * a.tokens;
   const int half = a.half;
-  const bool turns = PAIRS ? c < 2 * half : c < 2 * half && half > 0;
-  float C0[8], S0[8];
-  {
-    float sn = 0.f, cs = 1.f;
-    if (lane < half) {
-      const double t = (double)pos * (a.inv_freq[lane] * 0.15915494309189533577);
-      sincospif((float)(2.0 * (t - rint(t))), &sn, &cs);
-      sn *= a.scale;
-      cs *= a.scale;
-    }
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const int ch = c + k;
-      const int at = PAIRS ? ch >> 1 : ch < half ? ch : ch - half;
-      const float s = __shfl(sn, at & 63), o = __shfl(cs, at & 63);
-      const bool on = ch < 2 * half;
-      C0[k] = on ? o : 1.f;
-      S0[k] = !on ? 0.f : (PAIRS ? !(k & 1) : ch < half) ? -s : s;
-    }
-  }
-  // The lane and the first channel of the partners.
+  const int g = lane / LPH, c = 8 * (lane % LPH);
+  const bool turns = c < 2 * half;
   const int shift = c < half ? half : -half;
   const int partner = PAIRS || !turns ? lane : lane + shift / 8;
   const int pc = PAIRS || !turns ? c : c + shift;
+  // Groups of heads, and units of a token: uq of queries, then those of keys and values.
+  const int nq = (a.Hq + HPG - 1) / HPG, nk = (a.Hkv + HPG - 1) / HPG;
+  const int units = a.q_units + (nk + U::KV - 1) / U::KV;
 
-  int kind = -1;
-  bool normed = false;
-  float C[8], S[8];
-  for (; it < end; ++it) {
-    const Raw<T> r = next;
-    if (it + 1 < end) fetch(it + 1, &next);
-    const int now = kind_of(it), h = head_of(it, now);
-    const bool there = h < (now == 0 ? a.Hq : a.Hkv);
-    if (now != kind && now < 2) {
-      const float* w = a.weight[now];
-      normed = w != nullptr;
+  // Positions and words first, while nothing is written yet: they come through the scalar cache.
+  int32_t positions[kWaves], words[kWaves];
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) {
+    const bool there = i < a.tokens && first + i < a.n;
+    positions[i] = there ? a.positions[first + i] : -1;
+    words[i] = there ? a.words[first + i] : -1;
+  }
+  for (int i = threadIdx.x; i < 2 * D; i += 64 * kWaves)
+    if (const float* const w = i < D ? a.weight[0] : a.weight[1]) weights[i] = w[i & (D - 1)];
+  if (wave < a.tokens && lane < half) {
+    const int32_t pos = first + wave < a.n ? a.positions[first + wave] : 0;
+    const double t = (double)pos * (a.inv_freq[lane] * 0.15915494309189533577);
+    float sn, cs;
+    sincospif((float)(2.0 * (t - rint(t))), &sn, &cs);
+    cosines[wave][lane] = cs * a.scale;
+    sines[wave][lane] = sn * a.scale;
+  }
+  __syncthreads();
+
+  // Eight channels of head h of a token's rows (lanes behind the last head read that one's again).
+  const auto fetch = [&](int kind, int64_t token, int h, int heads, Raw<T>* r) {
+    const unsigned char* const row = a.src[kind] + token * a.stride[kind];
+    r->load(row + (unsigned)(min(h, heads - 1) * ROW + c * SZ));
+  };
+  const auto turn_of = [&](int at, int kind, bool normed, Turn* t) {
+    // (what is read for channels that do not turn is not used)
+    const int angle = (PAIRS ? c >> 1 : c < half ? c : c - half) & (PAIRS ? 60 : 56);
+#pragma unroll
+    for (int k = 0; k < 8; k += PAIRS ? 2 : 1) {
+      const bool on = PAIRS ? c + k < 2 * half : turns;
+      const float o = cosines[at][angle + (PAIRS ? k / 2 : k)], s = sines[at][angle + (PAIRS ? k / 2 : k)];
+      t->c[k] = on ? o : 1.f;
+      t->s[k] = !on ? 0.f : PAIRS || c < half ? -s : s;
+      if constexpr (PAIRS) {
+        t->c[k + 1] = t->c[k];
+        t->s[k + 1] = -t->s[k];
+      }
+    }
+    t->normed = normed;
+    if (normed) {
+      const float* const w = weights + kind * D;
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        C[k] = C0[k] * (normed ? w[c + k] : 1.f);
-        S[k] = S0[k] * (normed ? w[PAIRS ? c + (k ^ 1) : pc + k] : 1.f);
+        t->c[k] *= w[c + k];
+        t->s[k] *= w[PAIRS ? c + (k ^ 1) : pc + k];
       }
     }
-    kind = now;
-    Raw<T> y = r;
-    if (kind < 2) {
-      float x[8], p[8], z[8];
-      r.to(x);
-      if constexpr (PAIRS) {
+  };
+  const auto made = [&](const Raw<T>& r, const Turn& t) {
+    // Partners; a channel that does not turn takes nothing from another, not its infinity either.
+    float x[8], p[8], z[8];
+    r.to(x);
+    if constexpr (PAIRS) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) p[k] = x[k ^ 1];
-      } else {
-        Raw<T> o;
+      for (int k = 0; k < 8; ++k) p[k] = c + k < 2 * half ? x[k ^ 1] : 0.f;
+    } else {
+      Raw<T> o;
 #pragma unroll
-        for (int k = 0; k < Raw<T>::W; ++k) o.w[k] = (unsigned)__shfl((int)r.w[k], partner);
-        o.to(p);
+      for (int k = 0; k < Raw<T>::W; ++k) {
+        const unsigned w = (unsigned)__shfl((int)r.w[k], partner);
+        o.w[k] = turns ? w : 0;
       }
-      float rs = 1.f;
-      if (normed) {
-        float s = 0.f;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) s += x[k] * x[k];
-        rs = __builtin_amdgcn_rsqf(head_sum<D>(s) * (1.f / D) + a.eps);
-      }
-      // (a channel that does not turn takes nothing from another, not its infinity either)
-#pragma unroll
-      for (int k = 0; k < 8; ++k) z[k] = x[k] * C[k] + (c + k < 2 * half ? p[k] * S[k] : 0.f);
-      if (normed)
-#pragma unroll
-        for (int k = 0; k < 8; ++k) z[k] *= rs;
-      y.from(z);
+      o.to(p);
     }
-    if (kind == 0) {
-      if (there) y.store(a.q_out + ((int64_t)token * a.Hq + h) * ROW + c * (int)sizeof(T));
-    } else if constexpr (!FP4) {
-      if (there)
-        y.store(a.pool + ((((int64_t)(word >> 4) * a.Hkv + h) * 2 + (kind - 1)) * kPageTokens + (word & 15)) * ROW +
-                c * (int)sizeof(T));
+#pragma unroll
+    for (int k = 0; k < 8; ++k) z[k] = x[k] * t.c[k] + p[k] * t.s[k];
+    if (t.normed) {
+      float s = 0.f;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) s += x[k] * x[k];
+      const float rs = __builtin_amdgcn_rsqf(head_sum<D>(s) * (1.f / D) + a.eps);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) z[k] *= rs;
+    }
+    Raw<T> y;
+    y.from(z);
+    return y;
+  };
+  // Head h of a token's K or V to its slot.
+  const auto store_kv = [&](const Raw<T>& y, int32_t word, int h, bool value) {
+    if constexpr (!FP4) {
+      unsigned char* const page =
+          a.pool + ((int64_t)(word >> 4) * a.Hkv * (2 * kPageTokens) + ((value ? kPageTokens : 0) + (word & 15))) * ROW;
+      if (h < a.Hkv) y.store(page + (unsigned)(h * (2 * kPageTokens * ROW) + c * SZ));
     } else {
       unsigned code, byte;
       const unsigned w[4] = {y.w[0], y.w[1], y.w[2], y.w[3]};
       fp4_round(w, &code, &byte);
-      if (there) {
-        unsigned char* dst = a.pool + ((int64_t)(word >> 4) * a.Hkv + h) * Fp4<D>::PAGE;
-        store_codes<D>(dst, word & 15, c, kind == 2, code);
-        if ((c & 31) == 0) dst[fp4_scale<D>(word & 15, c, kind == 2)] = (unsigned char)byte;
+      if (h < a.Hkv) {
+        unsigned char* const dst = a.pool + ((int64_t)(word >> 4) * a.Hkv + h) * Fp4<D>::PAGE;
+        store_codes<D>(dst, word & 15, c, value, code);
+        if ((c & 31) == 0) dst[fp4_scale<D>(word & 15, c, value)] = (unsigned char)byte;
       }
+    }
+  };
+
+  // The units of the workgroup's tokens in turn; every wave takes each kind of unit in its turns.
+  for (int u = (int)(blockIdx.y * kWaves) + wave; u < units * a.tokens; u += kWaves * (int)gridDim.y) {
+    const int at = u / units;
+    const int64_t token = first + at;
+    if (token >= a.n) break;
+    const int unit = (u - at * units + at) % units;
+    const int32_t pos = at == 0 ? positions[0] : at == 1 ? positions[1] : at == 2 ? positions[2] : positions[3];
+    const int32_t word = at == 0 ? words[0] : at == 1 ? words[1] : at == 2 ? words[2] : words[3];
+    if (pos < 0) continue;
+    Raw<T> r[U::Q];
+    Turn t;
+    if (unit < a.q_units) {
+      const int i0 = unit * a.q_groups, n = min(a.q_groups, nq - i0);
+#pragma unroll
+      for (int i = 0; i < U::Q; ++i)
+        if (i < n) fetch(0, token, (i0 + i) * HPG + g, a.Hq, &r[i]);
+      turn_of(at, 0, a.weight[0] != nullptr, &t);
+#pragma unroll
+      for (int i = 0; i < U::Q; ++i)
+        if (i < n) {
+          const int h = (i0 + i) * HPG + g;
+          const Raw<T> y = made(r[i], t);
+          if (h < a.Hq) y.store(a.q_out + token * (a.Hq * ROW) + (unsigned)(h * ROW + c * SZ));
+        }
+    } else if (word >= 0 && (int64_t)word < a.num_slots) {
+      const int i0 = (unit - a.q_units) * U::KV, n = min(U::KV, nk - i0);
+#pragma unroll
+      for (int i = 0; i < U::KV; ++i)
+        if (i < n) {
+          fetch(1, token, (i0 + i) * HPG + g, a.Hkv, &r[i]);
+          fetch(2, token, (i0 + i) * HPG + g, a.Hkv, &r[U::KV + i]);
+        }
+      turn_of(at, 1, a.weight[1] != nullptr, &t);
+#pragma unroll
+      for (int i = 0; i < U::KV; ++i)
+        if (i < n) {
+          const int h = (i0 + i) * HPG + g;
+          store_kv(made(r[i], t), word, h, false);
+          store_kv(r[U::KV + i], word, h, true);
+        }
     }
   }
 }
 
 template <int D, class T, bool FP4>
-void launch(const QkvArgs& a, unsigned grid, bool pairs, hipStream_t stream) {
-  if (pairs) hipLaunchKernelGGL((k_qkv<D, T, FP4, true>), dim3(grid), dim3(64 * kWaves), 0, stream, a);
-  else hipLaunchKernelGGL((k_qkv<D, T, FP4, false>), dim3(grid), dim3(64 * kWaves), 0, stream, a);
+void launch(const QkvArgs& a, dim3 grid, bool pairs, hipStream_t stream) {
+  if (pairs) hipLaunchKernelGGL((k_qkv<D, T, FP4, true>), grid, dim3(64 * kWaves), 0, stream, a);
+  else hipLaunchKernelGGL((k_qkv<D, T, FP4, false>), grid, dim3(64 * kWaves), 0, stream, a);
 }
 template <int D>
-void launch(const QkvArgs& a, unsigned grid, int dtype, bool pairs, hipStream_t stream) {
+void launch(const QkvArgs& a, dim3 grid, int dtype, bool pairs, hipStream_t stream) {
   if (dtype == GA_F32) launch<D, float, false>(a, grid, pairs, stream);
   else if (dtype == GA_BF16) launch<D, __bf16, false>(a, grid, pairs, stream);
   else launch<D, __bf16, true>(a, grid, pairs, stream);
@@ -211,17 +261,17 @@ void launch(const QkvArgs& a, unsigned grid, int dtype, bool pairs, hipStream_t 
 
 hipError_t launch_qkv(const QkvArgs& args, int dim, int dtype, bool interleaved, hipStream_t stream) {
   QkvArgs a = args;
-  const int group = 512 / dim;
-  const int groups = (a.Hq + group - 1) / group + 2 * ((a.Hkv + group - 1) / group);
-  // Groups of heads a wave.
-  const int64_t most = (int64_t)groups * a.n / 8192;
-  a.per = (int32_t)(most < 1 ? 1 : most > groups ? groups : most);
-  a.parts = (groups + a.per - 1) / a.per;
-  const int64_t tasks = (int64_t)a.n * a.parts;
-  const int64_t grid = (tasks + kWaves - 1) / kWaves;
-  if (grid > 0x3fffffffLL / kWaves) return hipErrorInvalidValue;
-  if (dim == 64) launch<64>(a, (unsigned)grid, dtype, interleaved, stream);
-  else launch<128>(a, (unsigned)grid, dtype, interleaved, stream);
+  const int group = 512 / dim, nq = (a.Hq + group - 1) / group, nk = (a.Hkv + group - 1) / group;
+  const int q = dtype == GA_F32 ? Units<float>::Q : Units<__bf16>::Q, kv = dtype == GA_F32 ? Units<float>::KV : Units<__bf16>::KV;
+  a.q_units = (nq + q - 1) / q;
+  a.q_groups = (nq + a.q_units - 1) / a.q_units;
+  // Four tokens a workgroup where there are enough of them to fill the device, else one, its units on as many
+  // workgroups as they need.
+  a.tokens = a.n >= 4096 ? kWaves : 1;
+  const int units = a.q_units + (nk + kv - 1) / kv;
+  const dim3 grid((unsigned)((a.n + a.tokens - 1) / a.tokens), (unsigned)(a.tokens > 1 ? 1 : (units + kWaves - 1) / kWaves));
+  if (dim == 64) launch<64>(a, grid, dtype, interleaved, stream);
+  else launch<128>(a, grid, dtype, interleaved, stream);
   return hipGetLastError();
 }
 

@@ -13,38 +13,38 @@
 namespace ga {
 namespace {
 
-constexpr int kThreads = 256;
 constexpr int kMaxTile = 1024;
-constexpr int kAhead = 4;          // outputs of a thread whose loads are in flight together
+constexpr int kGroup = 16;         // lanes that walk a branch's path together
+
+typedef int i32x4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef long i64x2 __attribute__((ext_vector_type(2), aligned(8)));
 
 struct Two {
   int64_t n, x;
 };
 
-// Exclusive sums over the workgroup's threads (in thread order), and the total.
-__device__ __forceinline__ Two block_scan(Two v, Two* total) {
-  __shared__ Two wave_sum[kThreads / 64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  Two s = v;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int64_t n = __shfl_up(s.n, d), x = __shfl_up(s.x, d);
-    if (lane >= d) {
-      s.n += n;
-      s.x += x;
-    }
-  }
-  if (lane == 63) wave_sum[wave] = s;
-  __syncthreads();
-  Two before{0, 0}, all{0, 0};
-#pragma unroll
-  for (int w = 0; w < kThreads / 64; ++w) {
-    if (w == wave) before = all;
-    all.n += wave_sum[w].n;
-    all.x += wave_sum[w].x;
+// Exclusive sums of v over the workgroup's threads (in thread order), its total, and the total of w.
+template <int NT>
+__device__ __forceinline__ Two block_scan(Two v, Two* total, Two w, Two* other) {
+  __shared__ Two sums[NT / 64][2];
+  const int wave = threadIdx.x >> 6;
+  const Two s{wave_scan(v.n), wave_scan(v.x)}, t{wave_scan(w.n), wave_scan(w.x)};
+  if ((threadIdx.x & 63) == 63) {
+    sums[wave][0] = s;
+    sums[wave][1] = t;
   }
   __syncthreads();
+  Two before{0, 0}, all{0, 0}, rest{0, 0};
+#pragma unroll
+  for (int i = 0; i < NT / 64; ++i) {
+    if (i == wave) before = all;
+    all.n += sums[i][0].n;
+    all.x += sums[i][0].x;
+    rest.n += sums[i][1].n;
+    rest.x += sums[i][1].x;
+  }
   *total = all;
+  *other = rest;
   return {before.n + s.n - v.n, before.x + s.x - v.x};
 }
 
@@ -56,42 +56,32 @@ __device__ __forceinline__ int find(const int64_t* begin, int n, int64_t j) {
   return lo;
 }
 
-__device__ __forceinline__ int64_t old_offset(const PageTableArgs& a, int64_t s) {
-  const int64_t o = a.old_offsets[s];
-  return o < 0 ? 0 : o < a.n_old_pages ? o : a.n_old_pages;
+__device__ __forceinline__ int64_t held(const PageTableArgs& a, int64_t offset) {
+  return offset < 0 ? 0 : offset < a.n_old_pages ? offset : a.n_old_pages;
 }
-
 struct Need {
   int64_t pages, had;
 };
-__device__ __forceinline__ Need need_of(const PageTableArgs& a, int32_t s) {
-  const int32_t len = a.seg_len[s];
+__device__ __forceinline__ Need need_of(const PageTableArgs& a, int32_t len, int64_t had) {
   const int64_t want = ((int64_t)(len > 0 ? len : 0) + a.spare + kPageTokens - 1) / kPageTokens;
-  int64_t had = 0;
-  if (s < a.S_old) {
-    had = old_offset(a, s + 1) - old_offset(a, s);
-    had = had < 0 ? 0 : had;
-  }
+  had = had < 0 ? 0 : had;
   return {want > had ? want : had, had};
 }
+__device__ __forceinline__ Need need_of(const PageTableArgs& a, int32_t s) {
+  return need_of(a, a.seg_len[s], s < a.S_old ? held(a, a.old_offsets[s + 1]) - held(a, a.old_offsets[s]) : 0);
+}
 
-__global__ __launch_bounds__(kThreads) void k_page_table(PageTableArgs a) {
-  __shared__ int64_t begin[kMaxTile], old[kMaxTile], fresh[kMaxTile];
-  __shared__ int32_t had[kMaxTile];
+template <int NT>
+__global__ __launch_bounds__(NT) void k_page_table(PageTableArgs a) {
+  extern __shared__ int64_t lds[];
+  int64_t* const begin = lds;                        // of a segment's pages, among the tile's
+  int64_t* const old = begin + a.tile;               // its first old page
+  int64_t* const fresh = old + a.tile;               // the free page that its page 0 would be
+  int32_t* const had = reinterpret_cast<int32_t*>(fresh + a.tile);
   const int tid = threadIdx.x;
   const int64_t t0 = (int64_t)blockIdx.x * a.tile;
   const int n = (int)(a.S - t0 < a.tile ? a.S - t0 : a.tile);
-  // Pages, and new ones, of the segments before this workgroup's.
-  Two sum{0, 0};
-#pragma unroll 4
-  for (int64_t s = tid; s < t0; s += kThreads) {
-    const Need d = need_of(a, (int32_t)s);
-    sum.n += d.pages;
-    sum.x += d.pages - d.had;
-  }
-  Two before;
-  block_scan(sum, &before);
-  const int per = (a.tile + kThreads - 1) / kThreads;
+  const int per = (a.tile + NT - 1) / NT;
   Two mine{0, 0}, total;
   for (int k = 0; k < per; ++k) {
     const int i = tid * per + k;
@@ -99,18 +89,44 @@ __global__ __launch_bounds__(kThreads) void k_page_table(PageTableArgs a) {
       const Need d = need_of(a, (int32_t)(t0 + i));
       begin[i] = d.pages;
       had[i] = (int32_t)d.had;
+      old[i] = t0 + i < a.S_old ? held(a, a.old_offsets[t0 + i]) : 0;
       mine.n += d.pages;
       mine.x += d.pages - d.had;
     }
   }
-  Two at = block_scan(mine, &total);
+  // Pages, and new ones, of the segments before this workgroup's: four segments a thread at a time, those that had
+  // pages (up to `both`) and those that had none.
+  Two sum{0, 0}, before;
+  const int64_t both = (a.S_old < t0 ? a.S_old : t0) & ~3LL;
+  const auto add = [&](const Need& d) {
+    sum.n += d.pages;
+    sum.x += d.pages - d.had;
+  };
+#pragma unroll 2
+  for (int64_t s = 4 * tid; s < both; s += 4 * NT) {
+    const i32x4 len = *reinterpret_cast<const i32x4*>(a.seg_len + s);
+    const i64x2 lo = *reinterpret_cast<const i64x2*>(a.old_offsets + s);
+    const i64x2 hi = *reinterpret_cast<const i64x2*>(a.old_offsets + s + 2);
+    const int64_t o[5] = {held(a, lo[0]), held(a, lo[1]), held(a, hi[0]), held(a, hi[1]), held(a, a.old_offsets[s + 4])};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) add(need_of(a, len[k], o[k + 1] - o[k]));
+  }
+  const int64_t one = a.S_old < t0 ? a.S_old : t0, rest = one + ((t0 - one) & ~3LL);
+  if (both + tid < one) add(need_of(a, (int32_t)(both + tid)));
+#pragma unroll 2
+  for (int64_t s = one + 4 * tid; s < rest; s += 4 * NT) {
+    const i32x4 len = *reinterpret_cast<const i32x4*>(a.seg_len + s);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) add(need_of(a, len[k], 0));
+  }
+  if (rest + tid < t0) add(need_of(a, (int32_t)(rest + tid)));
+  Two at = block_scan<NT>(mine, &total, sum, &before);
   for (int k = 0; k < per; ++k) {
     const int i = tid * per + k;
     if (i < n) {
       const int64_t pages = begin[i];
       begin[i] = at.n;
-      old[i] = t0 + i < a.S_old ? old_offset(a, t0 + i) : 0;
-      fresh[i] = before.x + at.x - had[i];           // ... of page had[i], its first new one
+      fresh[i] = before.x + at.x - had[i];
       if (blockIdx.y == 0) a.offsets[t0 + i] = before.n + at.n;
       at.n += pages;
       at.x += pages - had[i];
@@ -120,75 +136,88 @@ __global__ __launch_bounds__(kThreads) void k_page_table(PageTableArgs a) {
   __syncthreads();
   const int64_t room = a.capacity - before.n;        // (may be negative)
   const int64_t end = total.n < room ? total.n : room;
-  const int64_t stride = (int64_t)gridDim.y * kThreads;
-  for (int64_t j0 = (int64_t)blockIdx.y * kThreads + tid; j0 < end; j0 += kAhead * stride) {
-    int32_t page[kAhead];
+  for (int64_t j = 4 * ((int64_t)blockIdx.y * NT + tid); j < end; j += 4 * NT * (int64_t)gridDim.y) {
+    int i = find(begin, n, j);
+    i32x4 page;
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      const int64_t j = j0 + k * stride;
-      page[k] = -1;
-      if (j < end) {
-        const int i = find(begin, n, j);
-        const int64_t p = j - begin[i];
-        const bool is_old = p < had[i];
-        const int64_t from = is_old ? old[i] + p : fresh[i] + p;
-        if (from < (is_old ? a.n_old_pages : a.n_free)) page[k] = (is_old ? a.old_pages : a.free_pages)[from];
-      }
+    for (int k = 0; k < 4; ++k) {
+      while (i + 1 < n && begin[i + 1] <= j + k) ++i;
+      const int64_t p = j + k - begin[i];
+      const bool is_old = p < had[i];
+      const int64_t from = p + (is_old ? old[i] : fresh[i]);
+      page[k] = j + k < end && from < (is_old ? a.n_old_pages : a.n_free) ? (is_old ? a.old_pages : a.free_pages)[from] : -1;
     }
-#pragma unroll
-    for (int k = 0; k < kAhead; ++k)
-      if (j0 + k * stride < end) a.pages[before.n + j0 + k * stride] = page[k];
+    int32_t* const out = a.pages + before.n + j;
+    if (j + 4 <= end) *reinterpret_cast<i32x4*>(out) = page;
+    else
+      for (int k = 0; k < (int)(end - j); ++k) out[k] = page[k];
   }
 }
 
-__device__ __forceinline__ int64_t count_of(const SlotMapArgs& a, int64_t b) {
-  if (!a.counts) return 1;
-  const int32_t c = a.counts[b];
-  return c > 0 ? c : 0;
-}
+__device__ __forceinline__ int64_t count_of(int32_t c) { return c > 0 ? c : 0; }
 
-__global__ __launch_bounds__(kThreads) void k_slot_map(SlotMapArgs a) {
-  __shared__ int64_t begin[kMaxTile], first[kMaxTile], last[kMaxTile], base[kMaxTile];
-  __shared__ int32_t token[kMaxTile];                // of the item's first row; may be below 0
+template <int NT>
+__global__ __launch_bounds__(NT) void k_slot_map(SlotMapArgs a) {
+  extern __shared__ int64_t lds[];
+  int64_t* const begin = lds;                        // of a branch's rows, among the tile's
+  int64_t* const first = begin + a.tile;             // its last segment's pages
+  int64_t* const last = first + a.tile;
+  int64_t* const base = last + a.tile;               // tokens of its other segments
+  int32_t* const token = reinterpret_cast<int32_t*>(base + a.tile);   // of its first row; may be below 0
   const int tid = threadIdx.x;
   const int32_t B = a.g.num_branches;
   const int64_t t0 = (int64_t)blockIdx.x * a.tile;
   const int n = (int)(B - t0 < a.tile ? B - t0 : a.tile);
-  const int per = (a.tile + kThreads - 1) / kThreads;
-  // The items' own loads first: three that depend on each other, beside the sum of the counts before them.
-  Two mine{0, 0}, total;
-  for (int k = 0; k < per; ++k) {
-    const int i = tid * per + k;
-    if (i < n) {
-      const int64_t c = count_of(a, t0 + i);
-      begin[i] = c;
-      mine.n += c;
-      const PathRange p = path_range(a.g, (int32_t)(t0 + i));
-      int64_t before = 0;
-      int32_t s = -1;
-      for (int64_t e = p.first; e < p.end; ++e) {
-        if (s >= 0 && s < a.g.num_segments) before += max(a.g.seg_len[s], 0);
-        s = a.g.path_segs[e];
-      }
-      const SegRange r = seg_range(a.g, s);
-      const bool known = s >= 0 && s < a.g.num_segments;
-      // (no segment: a token below 0 in every row)
-      const int64_t t = known ? (int64_t)r.len - c : -(int64_t)0x7fffffff;
-      token[i] = (int32_t)(t < -0x7fffffff ? -0x7fffffff : t);
-      first[i] = r.first;
-      last[i] = known ? r.end : r.first;
-      base[i] = before;
+  // Its branches' paths, by some lanes each.
+  const int lane = tid % kGroup;
+  for (int i0 = 0; i0 < n; i0 += NT / kGroup) {      // (whole waves go round, for the row operations)
+    const int i = i0 + tid / kGroup;
+    const bool there = i < n;
+    const int64_t c = there && a.counts ? count_of(a.counts[t0 + i]) : 1;
+    const PathRange p = there ? path_range(a.g, (int32_t)(t0 + i)) : PathRange{0, 0};
+    int64_t before = 0;
+    if (there && p.first >= p.end && lane == 0) {             // no segment: a token below 0 in every row
+      token[i] = -0x7fffffff;
+      first[i] = last[i] = 0;
     }
+    for (int64_t e = p.first + lane; e < p.end; e += kGroup) {
+      const int32_t s = a.g.path_segs[e];
+      const SegRange r = seg_range(a.g, s);
+      if (e + 1 < p.end) {
+        before += r.len;
+      } else {
+        const int64_t t = s >= 0 && s < a.g.num_segments ? r.len - c : -0x7fffffff;
+        token[i] = (int32_t)(t < -0x7fffffff ? -0x7fffffff : t);
+        first[i] = r.first;
+        last[i] = r.end;
+      }
+    }
+    if (there && lane == 0) begin[i] = c;
+    // (the sum of a group's lanes, in its last one)
+    add_lane<0x111, 0xf>(&before);
+    add_lane<0x112, 0xf>(&before);
+    add_lane<0x114, 0xf>(&before);
+    add_lane<0x118, 0xf>(&before);
+    if (there && lane == kGroup - 1) base[i] = before;
   }
   Two sum{0, 0}, before;
   if (a.counts) {
-#pragma unroll 4
-    for (int64_t b = tid; b < t0; b += kThreads) sum.n += count_of(a, b);
-    block_scan(sum, &before);
-  } else {
-    before = {t0, 0};
+    const int64_t whole = t0 & ~3LL;
+#pragma unroll 2
+    for (int64_t b = 4 * tid; b < whole; b += 4 * NT) {
+      const i32x4 c = *reinterpret_cast<const i32x4*>(a.counts + b);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) sum.n += count_of(c[k]);
+    }
+    if (whole + tid < t0) sum.n += count_of(a.counts[whole + tid]);
   }
-  Two at = block_scan(mine, &total);
+  __syncthreads();
+  const int per = (a.tile + NT - 1) / NT;
+  Two mine{0, 0}, total;
+  for (int k = 0; k < per; ++k)
+    if (tid * per + k < n) mine.n += begin[tid * per + k];
+  Two at = block_scan<NT>(mine, &total, sum, &before);
+  if (!a.counts) before = {t0, 0};
   auto held = [](int64_t x) { return (int32_t)(x < 0x7fffffff ? x : 0x7fffffff); };
   for (int k = 0; k < per; ++k) {
     const int i = tid * per + k;
@@ -204,58 +233,78 @@ __global__ __launch_bounds__(kThreads) void k_slot_map(SlotMapArgs a) {
   __syncthreads();
   const int64_t room = (int64_t)a.capacity - before.n;
   const int64_t rows = total.n < room ? total.n : room;
-  // The last items' workgroups write the padding behind the rows too.
+  // The last branches' workgroups write the padding behind the rows too.
   const int64_t end = closes ? room : rows;
-  const int64_t stride = (int64_t)gridDim.y * kThreads;
-  for (int64_t j0 = (int64_t)blockIdx.y * kThreads + tid; j0 < end; j0 += kAhead * stride) {
-    int32_t word[kAhead], pos[kAhead], branch[kAhead];
+  for (int64_t j = 4 * ((int64_t)blockIdx.y * NT + tid); j < end; j += 4 * NT * (int64_t)gridDim.y) {
+    i32x4 word, pos, branch;
+    int i = n > 0 && j < rows ? find(begin, n, j) : 0;
+    int64_t entry = -1;                              // of the table, whose page `page` is
+    int32_t page = -1;
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      const int64_t j = j0 + k * stride;
+    for (int k = 0; k < 4; ++k) {
       word[k] = pos[k] = branch[k] = -1;
-      if (j < rows) {
-        const int i = find(begin, n, j);
-        const int64_t t = token[i] + (j - begin[i]), p = base[i] + t;
+      if (j + k < rows) {
+        while (i + 1 < n && begin[i + 1] <= j + k) ++i;
+        const int64_t t = token[i] + (j + k - begin[i]), p = base[i] + t;
         if (t >= 0 && p < 0x80000000LL) {
           pos[k] = (int32_t)p;
           branch[k] = (int32_t)t0 + i;
-          const int32_t page = a.words ? page_of(a.g, first[i], last[i], (int32_t)t) : -1;
-          word[k] = page < 0 ? -1 : page * kPageTokens + (int32_t)(t & (kPageTokens - 1));
+          if (a.words) {
+            const int64_t at = first[i] + (t >> 4);
+            if (at != entry && at < last[i]) {
+              page = page_of(a.g, first[i], last[i], (int32_t)t);
+              entry = at;
+            }
+            word[k] = at < last[i] && page >= 0 ? page * kPageTokens + (int32_t)(t & (kPageTokens - 1)) : -1;
+          }
         }
       }
     }
-#pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      const int64_t j = j0 + k * stride;
-      if (j >= end) continue;
-      if (a.words) a.words[before.n + j] = word[k];
-      if (a.positions) a.positions[before.n + j] = pos[k];
-      if (a.branches) a.branches[before.n + j] = branch[k];
-    }
+    const int64_t out = before.n + j;
+    const auto put = [&](int32_t* to, const i32x4& v) {
+      if (!to) return;
+      if (j + 4 <= end) *reinterpret_cast<i32x4*>(to + out) = v;
+      else
+        for (int k = 0; k < (int)(end - j); ++k) to[out + k] = v[k];
+    };
+    put(a.words, word);
+    put(a.positions, pos);
+    put(a.branches, branch);
   }
 }
 
-// Items of a workgroup, and workgroups of the same items.
-dim3 tiles_of(int64_t items, int32_t* tile) {
-  const int64_t t = (items + 511) / 512;
+// Items of a workgroup, and workgroups of the same items: one for every four outputs a thread that the caller's
+// capacity lets expect, up to what fills the device.
+dim3 tiles_of(int64_t items, int64_t capacity, int threads, int32_t* tile) {
+  const int64_t most = threads == 256 ? 512 : 256, t = (items + most - 1) / most;
   *tile = (int32_t)(t < 1 ? 1 : t > kMaxTile ? kMaxTile : t);
   const int64_t tiles = items > 0 ? (items + *tile - 1) / *tile : 1;
-  return dim3((unsigned)tiles, (unsigned)(tiles < 512 ? 512 / tiles : 1));
+  const int64_t want = capacity / (tiles * 4 * threads), room = 2048 * 256 / threads / tiles;
+  const int64_t splits = want < room ? want : room;
+  return dim3((unsigned)tiles, (unsigned)(splits < 1 ? 1 : splits));
 }
+// From some thousand items on, the counts before a workgroup's are worth more threads.
+int threads_of(int64_t items) { return items > 4096 ? 1024 : 256; }
 
 }  // namespace
 
 hipError_t launch_page_table(const PageTableArgs& args, hipStream_t stream) {
   PageTableArgs a = args;
-  const dim3 grid = tiles_of(a.S, &a.tile);
-  hipLaunchKernelGGL(k_page_table, grid, dim3(kThreads), 0, stream, a);
+  const int threads = threads_of(a.S);
+  const dim3 grid = tiles_of(a.S, a.capacity, threads, &a.tile);
+  const size_t lds = (size_t)a.tile * 28;
+  if (threads == 256) hipLaunchKernelGGL(k_page_table<256>, grid, dim3(256), lds, stream, a);
+  else hipLaunchKernelGGL(k_page_table<1024>, grid, dim3(1024), lds, stream, a);
   return hipGetLastError();
 }
 
 hipError_t launch_slot_map(const SlotMapArgs& args, hipStream_t stream) {
   SlotMapArgs a = args;
-  const dim3 grid = tiles_of(a.g.num_branches, &a.tile);
-  hipLaunchKernelGGL(k_slot_map, grid, dim3(kThreads), 0, stream, a);
+  const int threads = threads_of(a.g.num_branches);
+  const dim3 grid = tiles_of(a.g.num_branches, a.capacity, threads, &a.tile);
+  const size_t lds = (size_t)a.tile * 36;
+  if (threads == 256) hipLaunchKernelGGL(k_slot_map<256>, grid, dim3(256), lds, stream, a);
+  else hipLaunchKernelGGL(k_slot_map<1024>, grid, dim3(1024), lds, stream, a);
   return hipGetLastError();
 }
 

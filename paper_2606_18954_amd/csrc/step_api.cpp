@@ -126,6 +126,7 @@ ga_status graphattn_qkv_append(void* kv_page_pool, const void* q, const void* k,
     return vfail(GA_EINVAL, "inv_freq must be 8-byte aligned, the weights 16-byte aligned");
   if (num_tokens < 0) return vfail(GA_EINVAL, "num_tokens is negative");
   if (num_tokens > (1 << 28)) return vfail(GA_EUNSUPPORTED, "%d tokens (> 2^28)", num_tokens);
+  if (params->num_q_heads > (1 << 14)) return vfail(GA_EUNSUPPORTED, "%d heads (> 2^14)", params->num_q_heads);
   if (num_tokens == 0) return GA_OK;
   if (!kv_page_pool || !q || !k || !v || !positions || !slot_words || !q_out)
     return vfail(GA_EINVAL, "device pointers must be non-NULL");
@@ -174,7 +175,7 @@ ga_status graphattn_process_logits(const void* logits, int64_t logits_stride, in
   if (out_f32 != 0 && out_f32 != 1) return vfail(GA_EINVAL, "out_f32 must be 0 or 1");
   if (rows < 0) return vfail(GA_EINVAL, "rows is negative");
   if (vocab < 1) return vfail(GA_EINVAL, "vocab %d (< 1)", vocab);
-  if (vocab > (1 << 30)) return vfail(GA_EUNSUPPORTED, "vocab %d (> 2^30)", vocab);
+  if (vocab > (1 << 28)) return vfail(GA_EUNSUPPORTED, "vocab %d (> 2^28)", vocab);
   if (logits_stride < vocab || out_stride < vocab) return vfail(GA_EINVAL, "a row stride is below vocab (%d)", vocab);
   if (rules->prompt_segments < 0 || rules->num_bias < 0 || rules->num_masks < 0)
     return vfail(GA_EINVAL, "a size of the rules is negative");

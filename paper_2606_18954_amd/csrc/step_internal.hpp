@@ -42,7 +42,8 @@ struct QkvArgs {
   int64_t num_slots;
   float eps, scale;
   int32_t n, Hq, Hkv, half;      // half: rotary_dim / 2
-  int32_t per, parts;            // groups of heads of a wave, waves of a token
+  int32_t q_units, q_groups;     // waves' shares of a token's queries, and groups of heads in each
+  int32_t tokens;                // of a workgroup
 };
 
 struct LogitArgs {
@@ -88,14 +89,33 @@ __device__ __forceinline__ int32_t page_of(const ga_device_graph& g, int64_t fir
   return page >= 0 && (int64_t)page < g.num_pages ? page : -1;
 }
 
-// Branch b's entries of path_segs.
+// Branch b's entries of path_segs: both ends within the array.
 struct PathRange {
   int64_t first, end;
 };
 __device__ __forceinline__ PathRange path_range(const ga_device_graph& g, int32_t b) {
   const int64_t first = g.path_offsets[b], e = g.path_offsets[b + 1];
-  if (first < 0) return {0, 0};
+  if (first < 0 || first > g.num_path_segs || e < first) return {0, 0};
   return {first, e < g.num_path_segs ? e : g.num_path_segs};
+}
+
+// Sums over a wave by row operations (the adds of a scan through lane exchanges wait for LDS twelve times, 2 us of a
+// small call): CTRL's lane, or nothing where a row or a mask leaves it out, is added.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ void add_lane(int64_t* v) {
+  const int lo = __builtin_amdgcn_update_dpp(0, (int)*v, CTRL, ROWS, 0xf, false);
+  const int hi = __builtin_amdgcn_update_dpp(0, (int)(*v >> 32), CTRL, ROWS, 0xf, false);
+  *v += (int64_t)(((uint64_t)(unsigned)hi << 32) | (unsigned)lo);
+}
+// The sum of the lanes up to and with this one.
+__device__ __forceinline__ int64_t wave_scan(int64_t v) {
+  add_lane<0x111, 0xf>(&v);                          // one lane up in rows of 16
+  add_lane<0x112, 0xf>(&v);
+  add_lane<0x114, 0xf>(&v);
+  add_lane<0x118, 0xf>(&v);
+  add_lane<0x142, 0xa>(&v);                          // the last lane of row 0 to row 1, of 2 to 3
+  add_lane<0x143, 0xc>(&v);                          // lane 31 to rows 2 and 3
+  return v;
 }
 
 }  // namespace

@@ -109,7 +109,7 @@ def test_process_logits_errors():
            dict(r=dict(bias_offsets=FAKE + 4)), dict(out=FAKE, so=200), dict(out=FAKE, dtype=G.GA_BF16, wide=1)]
     bad += [dict(g=_graph(**x)) for x in BAD_GRAPHS]
     _refused(call, {}, bad, [G.GA_EINVAL] * len(bad))
-    for change in (dict(dtype=G.GA_MXFP4), dict(dtype=7), dict(V=(1 << 30) + 1, si=1 << 31, so=1 << 31)):
+    for change in (dict(dtype=G.GA_MXFP4), dict(dtype=7), dict(V=(1 << 28) + 1, si=1 << 31, so=1 << 31)):
         assert call(**change) == G.GA_EUNSUPPORTED, change
     assert call(rows=0) == G.GA_OK and call(rows=0, x=None, out=None) == G.GA_OK
 

@@ -45,8 +45,8 @@ def driver(tmp_path_factory):
     for name in SOURCES + HEADERS:
         with open(os.path.join(CSRC, name)) as f:
             text = f.read().replace('#include "../../include/', '#include "')
-        text = re.sub(r"extern __shared__ unsigned (\w+)\[\];",
-                      r"unsigned* \1 = static_cast<unsigned*>(emu::dynamic_lds());", text)
+        text = re.sub(r"extern __shared__ (unsigned|int64_t) (\w+)\[\];",
+                      r"\1* \2 = static_cast<\1*>(emu::dynamic_lds());", text)
         assert "asm volatile" not in text, name
         (out / name).write_text(text)
     (out / "shim.hpp").write_text(SHIM)
