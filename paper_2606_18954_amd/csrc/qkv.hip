@@ -23,7 +23,7 @@ constexpr int kWaves = 4;          // of a workgroup
 // Groups of heads that a wave takes at once, all of their loads ahead of the first store: of q, or of k and of v.
 template <class T>
 struct Units {
-  static constexpr int Q = sizeof(T) == 4 ? 3 : 5, KV = sizeof(T) == 4 ? 1 : 2;
+  static constexpr int Q = sizeof(T) == 4 ? 2 : 3, KV = 1;
 };
 
 __device__ __forceinline__ float bf16_lo(unsigned w) { return __builtin_bit_cast(float, w << 16); }
@@ -46,10 +46,13 @@ struct Raw {
       for (int k = 0; k < 4; ++k) w[4 * i + k] = v[k];
     }
   }
-  __device__ __forceinline__ void store(unsigned char* p) const {
+  __device__ __forceinline__ void store(unsigned char* p, bool past) const {
 #pragma unroll
-    for (int i = 0; i < W / 4; ++i)
-      reinterpret_cast<u32x4*>(p)[i] = u32x4{w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]};
+    for (int i = 0; i < W / 4; ++i) {
+      const u32x4 v = {w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]};
+      if (past) __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(p) + i);
+      else reinterpret_cast<u32x4*>(p)[i] = v;
+    }
   }
   __device__ __forceinline__ void to(float (&x)[8]) const {
 #pragma unroll
@@ -188,7 +191,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_qkv(QkvArgs a) {
     if constexpr (!FP4) {
       unsigned char* const page =
           a.pool + ((int64_t)(word >> 4) * a.Hkv * (2 * kPageTokens) + ((value ? kPageTokens : 0) + (word & 15))) * ROW;
-      if (h < a.Hkv) y.store(page + (unsigned)(h * (2 * kPageTokens * ROW) + c * SZ));
+      if (h < a.Hkv) y.store(page + (unsigned)(h * (2 * kPageTokens * ROW) + c * SZ), a.past);
     } else {
       unsigned code, byte;
       const unsigned w[4] = {y.w[0], y.w[1], y.w[2], y.w[3]};
@@ -210,7 +213,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_qkv(QkvArgs a) {
     const int32_t pos = at == 0 ? positions[0] : at == 1 ? positions[1] : at == 2 ? positions[2] : positions[3];
     const int32_t word = at == 0 ? words[0] : at == 1 ? words[1] : at == 2 ? words[2] : words[3];
     if (pos < 0) continue;
-    Raw<T> r[U::Q];
+    Raw<T> r[U::Q > 2 * U::KV ? U::Q : 2 * U::KV];
     Turn t;
     if (unit < a.q_units) {
       const int i0 = unit * a.q_groups, n = min(a.q_groups, nq - i0);
@@ -223,7 +226,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_qkv(QkvArgs a) {
         if (i < n) {
           const int h = (i0 + i) * HPG + g;
           const Raw<T> y = made(r[i], t);
-          if (h < a.Hq) y.store(a.q_out + token * (a.Hq * ROW) + (unsigned)(h * ROW + c * SZ));
+          if (h < a.Hq) y.store(a.q_out + token * (a.Hq * ROW) + (unsigned)(h * ROW + c * SZ), a.past);
         }
     } else if (word >= 0 && (int64_t)word < a.num_slots) {
       const int i0 = (unit - a.q_units) * U::KV, n = min(U::KV, nk - i0);
@@ -265,6 +268,8 @@ hipError_t launch_qkv(const QkvArgs& args, int dim, int dtype, bool interleaved,
   const int q = dtype == GA_F32 ? Units<float>::Q : Units<__bf16>::Q, kv = dtype == GA_F32 ? Units<float>::KV : Units<__bf16>::KV;
   a.q_units = (nq + q - 1) / q;
   a.q_groups = (nq + a.q_units - 1) / a.q_units;
+  // What is written goes past the caches where they could not hold it for the attention that follows.
+  a.past = (int64_t)a.n * (a.Hq + 2 * a.Hkv) * dim * (dtype == GA_F32 ? 4 : 2) > (32 << 20);
   // Four tokens a workgroup where there are enough of them to fill the device, else one, its units on as many
   // workgroups as they need.
   a.tokens = a.n >= 4096 ? kWaves : 1;

@@ -580,13 +580,14 @@ class QKTransform:
         self.ref = ctypes.byref(self.c)
 
 
-def _rows(t, n: int, heads: int, dim: int, dtype) -> tuple:
+def _rows(t, shape: tuple, dtype) -> tuple:
     """(pointer, values from a token's heads to the next one's) of rows [n, heads, dim]; the heads of a token lie one
     behind the other."""
-    if t.dtype != dtype or tuple(t.shape) != (n, heads, dim):
-        raise ValueError(f"q, K and V rows beside this pool are {dtype} [tokens, heads, {dim}]")
+    if t.dtype != dtype or t.shape != shape:
+        raise ValueError(f"q, K and V rows beside this pool are {dtype} [tokens, heads, {shape[2]}]")
+    n, heads, dim = shape
     token, head, channel = t.stride()
-    if n and (channel != 1 or (heads > 1 and head != dim)):
+    if (channel != 1 or (heads > 1 and head != dim)) and n:
         raise ValueError("the heads of a token must lie one behind the other")
     if not t.is_cuda:
         raise ValueError("tensors passed to the library must live on the GPU")
@@ -610,7 +611,10 @@ def qkv_append(pool, q, k, v, positions, slot_words, transform: QKTransform, par
         q_out = torch.zeros((n, Hq, D), dtype=row, device=q.device)
     what = "positions and slot_words must be int32, one per token"
     pw, ww = _array(positions, torch.int32, n, what), _array(slot_words, torch.int32, n, what)
-    (qp, qs), (kp, ks), (vp, vs) = (_rows(t, n, h, D, row) for t, h in ((q, Hq), (k, Hkv), (v, Hkv)))
+    shape = (n, Hkv, D)
+    qp, qs = _rows(q, (n, Hq, D), row)
+    kp, ks = _rows(k, shape, row)
+    vp, vs = _rows(v, shape, row)
     op = _array(q_out, row, n * Hq * D, "q_out must be [tokens, Hq, D] of q's type, contiguous")
     _check(lib.graphattn_qkv_append(_dev_ptr(pool), qp, kp, vp, qs, ks, vs, pw, ww, n, op, transform.ref,
                                     ctypes.byref(params), handle))

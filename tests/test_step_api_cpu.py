@@ -207,11 +207,11 @@ def test_qkv_append_refusals(dtype):
             G.qkv_append(**{**good, **change})
     for t, n, h in ((rows[:, :4].to(other), 5, 4), (rows[:, :3], 5, 4), (rows[:4, :4], 5, 4), (rows[..., :32], 5, 8)):
         with pytest.raises(ValueError, match="rows beside"):
-            G._rows(t, n, h, 64, row)
+            G._rows(t, (n, h, 64), row)
     wide = torch.zeros(5, 4, 128, dtype=row)
     for t in (wide[..., ::2], wide[..., :64], torch.zeros(5, 64, 4, dtype=row).transpose(1, 2)):
         with pytest.raises(ValueError, match="one behind the other"):
-            G._rows(t, 5, 4, 64, row)
+            G._rows(t, (5, 4, 64), row)
 
 
 def test_logits_refusals(graph):
