@@ -23,8 +23,8 @@ constexpr int kThreads = 512;
 constexpr int kPath = 64;          // segments of a path taken at once
 constexpr int kAhead = 2;          // fours of tokens of a thread whose loads are in flight together
 constexpr int kBias = 512;         // biases of a row that LDS holds; a longer list is looked up in memory
-// Tokens of a slice, so that four workgroups share a CU's LDS: 38 KB of counts, or 34 and the biases.
-constexpr int kMaxSlice = 19456, kMaxSliceBiased = 17408;
+// Tokens of a slice, so that four workgroups share a CU's LDS: 38 KB of counts, or 33 and the biases.
+constexpr int kMaxSlice = 19456, kMaxSliceBiased = 16896;
 
 typedef unsigned u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 typedef int i32x4_any __attribute__((ext_vector_type(4), aligned(4)));
@@ -86,6 +86,21 @@ __device__ __forceinline__ float sum_of(const int32_t* tokens, const float* valu
   }
   float s = 0.f;
   for (; lo < n && tokens[lo] == v; ++lo) s += values[lo];
+  return s;
+}
+
+// The same from an entry at or before its first.
+struct alignas(8) Bias {
+  int32_t token;
+  float value;
+};
+__device__ __forceinline__ float sum_from(const Bias* list, int at, int n, int v) {
+  float s = 0.f;
+  for (; at < n; ++at) {
+    const Bias b = list[at];
+    if (b.token > v) break;
+    s += b.token == v ? b.value : 0.f;
+  }
   return s;
 }
 
@@ -161,13 +176,13 @@ __global__ __launch_bounds__(kThreads, 8) void k_logits(LogitArgs a) {
   row.in = a.in + r * a.in_stride * (int64_t)sizeof(TI);
   row.out = a.out + r * a.out_stride * (int64_t)sizeof(TO);
   Values<TI, E> x[LOADS];
+  const auto fetch_one = [&](Values<TI, E>* to, int v, int hi) {
+    if (v + E <= hi) to->load(row.in, v);
+    else to->load_some(row.in, v, hi - v);
+  };
   const auto fetch = [&](int v0, int hi) {
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      const int v = v0 + E * (tid + i * kThreads);
-      if (v + E <= hi) x[i].load(row.in, v);
-      else x[i].load_some(row.in, v, hi - v);
-    }
+    for (int i = 0; i < LOADS; ++i) fetch_one(&x[i], v0 + E * (tid + i * kThreads), hi);
   };
   row.rep = a.rules.repetition ? a.rules.repetition[r] : 1.f;
   row.inv_rep = 1.f / row.rep;
@@ -220,14 +235,13 @@ __global__ __launch_bounds__(kThreads, 8) void k_logits(LogitArgs a) {
   const bool wide = said > 0x3fff;
   const int n_bias = (int)min(bias_end - bias_first, (int64_t)0x7fffffff);
   const bool near = biased && n_bias <= kBias;
-  int32_t* const near_tokens = reinterpret_cast<int32_t*>(counts + a.slice / 2 + 16);
-  float* const near_values = reinterpret_cast<float*>(near_tokens + kBias);
+  Bias* const near_list = reinterpret_cast<Bias*>(counts + a.slice / 2 + 16);
+  unsigned short* const near_first = reinterpret_cast<unsigned short*>(near_list + kBias);
 
   // The slice [lo, hi), with counts of 16 or 32 bits.
   const auto pass = [&](auto wide_counts, int lo, int hi) {
     constexpr bool WIDE = decltype(wide_counts)::value;
     if (lo != lo0) {
-      fetch(lo, hi);
       __syncthreads();
       clear();
       __syncthreads();
@@ -295,25 +309,22 @@ __global__ __launch_bounds__(kThreads, 8) void k_logits(LogitArgs a) {
     if (biased)
       for (unsigned e = tid; e < (unsigned)n_bias; e += kThreads) {
         const int v = a.rules.bias_tokens[bias_first + e];
-        if (v >= lo && v < hi) flag(v - lo, 0x4000u);
-        if (near) {
-          near_tokens[e] = v;
-          near_values[e] = a.rules.bias_values[bias_first + e];
+        if (near) near_list[e] = {v, a.rules.bias_values[bias_first + e]};
+        if (v >= lo && v < hi) {
+          flag(v - lo, 0x4000u);
+          // The first of 32 tokens says where in the list theirs are.
+          const int before = e ? a.rules.bias_tokens[bias_first + e - 1] : -1;
+          if (near && (before < lo || before >> 5 != v >> 5)) near_first[(v - lo) >> 5] = (unsigned short)e;
         }
       }
     if (flags) __syncthreads();
 
-    for (int v0 = lo; v0 < hi; v0 += E * LOADS * kThreads) {
-      if (v0 != lo) fetch(v0, hi);
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i) {
-        const int v = v0 + E * (tid + i * kThreads), m = min(E, hi - v);
-        if (m <= 0) continue;
+    const auto work = [&](const Values<TI, E>& in, int v, int m) {
         unsigned allowed = ~0u;
         if (row.mask) allowed = row.mask[v >> 5] >> (v & 31);
         float z[E];
 #pragma unroll
-        for (int k = 0; k < E; ++k) z[k] = x[i].at(k);
+        for (int k = 0; k < E; ++k) z[k] = in.at(k);
         if (flags) {
           constexpr int W = WIDE ? E : E / 2;
           const unsigned* const word = counts + (WIDE ? v - lo : (v - lo) >> 1);
@@ -329,7 +340,7 @@ __global__ __launch_bounds__(kThreads, 8) void k_logits(LogitArgs a) {
             for (some &= (1u << m) - 1; some; some &= some - 1) {
               const int j = __builtin_ctz(some);
               const float bias =
-                  near ? sum_of(near_tokens, near_values, n_bias, v + j)
+                  near ? sum_from(near_list, near_first[(v + j - lo) >> 5], n_bias, v + j)
                        : sum_of(a.rules.bias_tokens + bias_first, a.rules.bias_values + bias_first, n_bias, v + j);
 #pragma unroll
               for (int k = 0; k < E; ++k) z[k] += j == k ? bias : 0.f;
@@ -357,15 +368,29 @@ __global__ __launch_bounds__(kThreads, 8) void k_logits(LogitArgs a) {
           for (int k = 0; k < E; ++k)
             if (k < m) reinterpret_cast<TO*>(row.out)[v + k] = (TO)z[k];
         }
+    };
+    if constexpr (WIDE) {
+      // (rare: one load at a time)
+      for (int v = lo + E * tid; v < hi; v += E * kThreads) {
+        fetch_one(&x[0], v, hi);
+        work(x[0], v, min(E, hi - v));
+      }
+    } else {
+      for (int v0 = lo; v0 < hi; v0 += E * LOADS * kThreads) {
+        if (v0 != lo) fetch(v0, hi);
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+          const int v = v0 + E * (tid + i * kThreads), m = min(E, hi - v);
+          if (m > 0) work(x[i], v, m);
+        }
       }
     }
   };
   if (!wide) {
     pass(std::false_type{}, lo0, hi0);
   } else {
-    const int mid = min(lo0 + (a.slice / 2 + 31) / 32 * 32, hi0);
-    pass(std::true_type{}, lo0, mid);
-    if (mid < hi0) pass(std::true_type{}, mid, hi0);
+    const int step = (a.slice / 2 + 31) / 32 * 32;
+    for (int lo = lo0; lo < hi0; lo += step) pass(std::true_type{}, lo, min(lo + step, hi0));
   }
 }
 
@@ -384,7 +409,7 @@ hipError_t launch_logits(const LogitArgs& args, bool in_f32, bool out_f32, hipSt
   a.rows_per_xcd = (a.rows + 7) / 8;
   const int64_t grid = (int64_t)a.rows_per_xcd * 8 * a.parts;
   if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
-  const size_t lds = (size_t)a.slice * 2 + 64 + (biased ? kBias * 8 : 0);
+  const size_t lds = (size_t)a.slice * 2 + 64 + (biased ? kBias * 8 + a.slice / 16 : 0);
   const dim3 g((unsigned)grid), t(kThreads);
   if (in_f32) hipLaunchKernelGGL((k_logits<float, float>), g, t, lds, stream, a);
   else if (out_f32) hipLaunchKernelGGL((k_logits<__bf16, float>), g, t, lds, stream, a);
