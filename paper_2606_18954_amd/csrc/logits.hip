@@ -19,12 +19,14 @@
 namespace ga {
 namespace {
 
-constexpr int kThreads = 512;
+constexpr int kThreads = 1024;
 constexpr int kPath = 64;          // segments of a path taken at once
 constexpr int kAhead = 2;          // fours of tokens of a thread whose loads are in flight together
 constexpr int kBias = 512;         // biases of a row that LDS holds; a longer list is looked up in memory
-// Tokens of a slice, so that four workgroups share a CU's LDS: 38 KB of counts, or 33 and the biases.
-constexpr int kMaxSlice = 19456, kMaxSliceBiased = 16896;
+// Tokens of a slice, so that two workgroups share a CU's LDS: 76 KB of counts, or 72 and the biases.  (With half the
+// threads and slices, and four workgroups, every row's path is read twice as often: logits of 1024 rows of four drafted
+// tokens a branch over 65024 tokens, contexts of some 14000, take 117 us, not 99; 128 rows of 50001 15.6, not 14.6.)
+constexpr int kMaxSlice = 38912, kMaxSliceBiased = 36864;
 
 typedef unsigned u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 typedef int i32x4_any __attribute__((ext_vector_type(4), aligned(4)));
@@ -402,7 +404,7 @@ hipError_t launch_logits(const LogitArgs& args, bool in_f32, bool out_f32, hipSt
   const bool biased = a.rules.bias_offsets != nullptr;
   const int64_t largest = biased ? kMaxSliceBiased : kMaxSlice;
   const int64_t least = (a.vocab + largest - 1) / largest, most = (a.vocab + 2047) / 2048;
-  int64_t parts = (1024 + a.rows - 1) / a.rows;
+  int64_t parts = (512 + a.rows - 1) / a.rows;
   parts = parts < least ? least : parts > most ? most : parts;
   a.slice = (int32_t)(((a.vocab + parts - 1) / parts + 31) / 32 * 32);
   a.parts = (a.vocab + a.slice - 1) / a.slice;

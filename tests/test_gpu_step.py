@@ -457,3 +457,79 @@ def test_a_rollout_by_these_calls(dtype):
             seen = [(t, True) for t in said[0]] + [(t, False) for t in said[1 + b]]
             want, size = S.logits_row(logits[b].double().cpu().numpy(), seen, float(r[b]), float(f[b]))
             assert (np.abs(z[b].double().cpu().numpy() - want) <= 2.0 ** -21 * size).all()
+
+
+def test_many_rows_of_drafts():
+    """More rows than the device takes at once: several positions a branch, in order and not, with padding between them."""
+    require_gpu()
+    rng = np.random.default_rng(44)
+    g = U.random_graph(rng, 12)
+    c = U.logits_case(rng, g, 1300, 1201, "bf16", rules="rfptbm", biases=2)
+    c["branches"][:] = np.repeat(rng.integers(-1, len(g["po"]) - 1, 260), 5)
+    c["positions"][:] = (rng.integers(0, 60, 260)[:, None] + np.cumsum(rng.choice([0, 1, 2, 40, -3], (260, 5)), 1)).reshape(-1)
+    s = Logits(c)
+    U.check_logits(c, host(s.call()), s.before)
+
+
+def test_offsets_beyond_32_bits():
+    """Rows of logits, tokens of a projection and pages behind 4 GiB."""
+    require_gpu()
+    rng = np.random.default_rng(45)
+    g = U.graph([40, 3], [[0], [0, 1]], rng)
+    rows, V = 9000, 152064
+    x = torch.zeros(rows, V, device="cuda")                # 5.5 GB
+    last = torch.randn(2, V, device="cuda")
+    x[-2:] = last
+    branches = torch.full((rows,), -1, dtype=torch.int32, device="cuda")
+    branches[-2:] = dev(np.array([0, 1], np.int32))
+    c = U.logits_case(rng, g, 2, V, "f32", rules="rfptm", drafts=False)
+    c["logits"] = host(last)
+
+    def long(a):
+        """A rule's values in the last two rows of many."""
+        t = torch.zeros(rows, dtype=torch.float32 if a.dtype == np.float32 else torch.int32, device="cuda")
+        t[-2:] = dev(a)
+        return t
+    rules = G.LogitRules(long(c["rep"]), long(c["freq"]), long(c["pres"]), long(c["temp"]), c["prompt"], masks=dev(c["masks"][0]),
+                         row_mask=long(c["masks"][1]))
+    out = G.process_logits(x, rules, device_graph(g), dev(c["ids"]), branches, None, x)
+    U.check_logits(c, host(out[-2:]), c["logits"])
+    assert not out[:-2].any()
+    del x, out
+    # A pool of 5 GB, its last pages; rows 2 MB apart, the last beyond 4 GiB.
+    n, Hq, Hkv, D, far = 2100, 2, 2, 128, 1 << 20
+    c = U.qkv_case(rng, n, Hq, Hkv, D, "bf16", D)
+    c["num_pages"] = 5 * (1 << 30) // (Hkv * 2 * 16 * D * 2)
+    c["words"] = (16 * c["num_pages"] - 1 - rng.permutation(4 * n)[:n]).astype(np.int32)
+    c["positions"][:] = rng.integers(0, 9000, n)
+    rows = torch.zeros(n, far, dtype=torch.bfloat16, device="cuda")
+    rows[:, :6 * D] = dev(c["rows"])
+    body = rows[:, :6 * D].view(n, 6, D)
+    params = G.make_params(Hq, Hkv, D, c["num_pages"], "bf16")
+    pool = G.empty_pool(params)
+    transform = G.QKTransform(D, dev(c["inv_freq"]), False, *(dev(w) for w in c["weights"]), c["eps"])
+    q = G.qkv_append(pool, *body.split([Hq, Hkv, Hkv], 1), dev(c["positions"]), dev(c["words"]), transform, params)
+    every = np.ones(n, dtype=bool)
+    U.check_rows(host(q), U.qkv_parts(c)[0], c, c["weights"][0], every)
+    k, v = G.kv_read(pool, dev(c["words"]), params)
+    U.check_rows(host(k), U.qkv_parts(c)[1], c, c["weights"][1], every)
+    np.testing.assert_array_equal(host(v), U.qkv_parts(c)[2])
+
+
+def test_two_calls_at_once():
+    """The same call's arrays on two streams: calls keep nothing, so neither disturbs the other."""
+    require_gpu()
+    rng = np.random.default_rng(46)
+    g = U.random_graph(rng, 12)
+    a, b = (Logits(U.logits_case(rng, g, 600, 20001, "f32", rules="rfptb")) for _ in range(2))
+    p, q = (U.slot_case(rng) for _ in range(2))
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for s, x in zip(streams, (a, b)):
+            x.call(s)
+    torch.cuda.synchronize()
+    for x in (a, b):
+        U.check_logits(x.c, host(x.out_buffer), x.before)
+    for c in (p, q):
+        U.check_slots(c, *run_slots(c))
