@@ -48,7 +48,8 @@ typedef struct {
  * from capacity on are not written.  old_offsets [num_old_segments + 1], old_pages [num_old_pages] and
  * free_pages [num_free]: device; num_old_segments in [0, num_segments], 0 for a table that starts (old_offsets
  * and old_pages may be NULL).  old_offsets holds what an earlier call wrote (or any CSR from 0 on); a value outside
- * [0, num_old_pages] is taken as the nearer end.  Outputs must not overlap the inputs. */
+ * [0, num_old_pages] is taken as the nearer end.  GA_EINVAL where an output overlaps
+ * another array. */
 ga_status graphattn_page_table(const int32_t* seg_len, int32_t num_segments, int32_t spare_tokens,
                                const int64_t* old_offsets, const int32_t* old_pages,
                                int32_t num_old_segments, int64_t num_old_pages,
@@ -68,7 +69,8 @@ ga_status graphattn_page_table(const int32_t* seg_len, int32_t num_segments, int
  *   branches      [capacity] device int32: b
  * Rows from the total to capacity are padding, as are the tokens of a branch without a path, whose last segment
  * is outside the graph, with t < 0 or with a position of 2^31 or more: slot word, position and branch are -1.
- * Rows from capacity on are not written.  slot_words, positions and branches may each be NULL.  Branches that
+ * Rows from capacity on are not written.  slot_words, positions and branches may each be NULL; GA_EINVAL where an output
+ * overlaps another array.  Branches that
  * end in the same segment name the same slots (graphattn_kv_append wants them once). */
 ga_status graphattn_slot_map(const ga_device_graph* graph, const int32_t* new_counts,
                              int32_t* token_offsets, int32_t* slot_words, int32_t* positions,

@@ -30,6 +30,22 @@ bool misaligned(size_t to, std::initializer_list<const void*> ptrs) {
   return all & (to - 1);
 }
 
+// Whether two arrays share bytes.
+struct Range {
+  const void* p;
+  int64_t bytes;
+};
+bool overlap(Range a, Range b) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+  return a.p && b.p && a.bytes > 0 && b.bytes > 0 && x < y + (uintptr_t)b.bytes && y < x + (uintptr_t)a.bytes;
+}
+bool overlap(std::initializer_list<Range> outs, std::initializer_list<Range> ins) {
+  for (const Range& a : outs)
+    for (const Range& b : ins)
+      if (overlap(a, b)) return true;
+  return false;
+}
+
 ga_status check_graph(const ga_device_graph* g) {
   if (!g) return vfail(GA_EINVAL, "graph is NULL");
   if (g->num_segments < 0 || g->num_branches < 0 || g->num_table_pages < 0 || g->num_path_segs < 0 ||
@@ -64,6 +80,13 @@ ga_status graphattn_page_table(const int32_t* seg_len, int32_t num_segments, int
     return vfail(GA_EINVAL, "device pointers must be non-NULL");
   if (misaligned(4, {seg_len, old_pages, free_pages, seg_pages}) || misaligned(8, {old_offsets, seg_page_offsets}))
     return vfail(GA_EINVAL, "arrays must be aligned to their elements");
+  const Range offsets{seg_page_offsets, 8 * ((int64_t)num_segments + 1)}, pages{seg_pages, 4 * capacity};
+  if (overlap({offsets, pages}, {{seg_len, 4 * (int64_t)num_segments},
+                                 {old_offsets, num_old_segments ? 8 * ((int64_t)num_old_segments + 1) : 0},
+                                 {old_pages, 4 * num_old_pages},
+                                 {free_pages, 4 * num_free}}) ||
+      overlap(offsets, pages))
+    return vfail(GA_EINVAL, "the new table overlaps another array");
   ga::PageTableArgs a{};
   a.seg_len = seg_len;
   a.old_offsets = old_offsets;
@@ -91,6 +114,16 @@ ga_status graphattn_slot_map(const ga_device_graph* graph, const int32_t* new_co
   if (!token_offsets) return vfail(GA_EINVAL, "token_offsets is NULL");
   if (misaligned(4, {new_counts, token_offsets, slot_words, positions, branches}))
     return vfail(GA_EINVAL, "new_counts and the outputs must be 4-byte aligned");
+  const int64_t B = graph->num_branches, rows = 4 * (int64_t)capacity;
+  const Range offsets{token_offsets, 4 * (B + 1)}, words{slot_words, rows}, pos{positions, rows}, br{branches, rows};
+  if (overlap({offsets, words, pos, br}, {{new_counts, 4 * B},
+                                          {graph->seg_len, 4 * (int64_t)graph->num_segments},
+                                          {graph->seg_page_offsets, 8 * ((int64_t)graph->num_segments + 1)},
+                                          {graph->seg_pages, 4 * graph->num_table_pages},
+                                          {graph->path_offsets, 8 * (B + 1)},
+                                          {graph->path_segs, 4 * graph->num_path_segs}}) ||
+      overlap({offsets}, {words, pos, br}) || overlap({words}, {pos, br}) || overlap(pos, br))
+    return vfail(GA_EINVAL, "an output overlaps another array");
   ga::SlotMapArgs a{};
   a.g = *graph;
   a.counts = new_counts;
@@ -138,8 +171,13 @@ ga_status graphattn_qkv_append(void* kv_page_pool, const void* q, const void* k,
   const int64_t stride[3] = {q_stride, k_stride, v_stride};
   for (const int64_t s : stride)
     if (s < 0 || s * elt % 16) return vfail(GA_EINVAL, "strides must be >= 0 and multiples of 16 bytes");
-  if (q_out == q && q_stride != (int64_t)params->num_q_heads * D && num_tokens > 1)
-    return vfail(GA_EINVAL, "q_out may be q only where q's rows lie one behind the other");
+  const int64_t n = num_tokens, q_row = (int64_t)params->num_q_heads * D, kv_row = (int64_t)params->num_kv_heads * D;
+  const Range out{q_out, n * q_row * elt};
+  const bool in_place = q_out == q && (q_stride == q_row || n == 1);
+  if (overlap({out}, {{q, in_place ? 0 : ((n - 1) * q_stride + q_row) * elt},
+                      {k, ((n - 1) * k_stride + kv_row) * elt},
+                      {v, ((n - 1) * v_stride + kv_row) * elt}}))
+    return vfail(GA_EINVAL, "q_out overlaps the rows that are read; it may be q itself where q's rows lie one behind the other");
   ga::QkvArgs a{};
   a.src[0] = static_cast<const unsigned char*>(q);
   a.src[1] = static_cast<const unsigned char*>(k);
@@ -203,8 +241,11 @@ ga_status graphattn_process_logits(const void* logits, int64_t logits_stride, in
   const bool in_f32 = dtype == GA_F32, wide = in_f32 || out_f32;
   if (misaligned(in_f32 ? 4 : 2, {logits}) || misaligned(wide ? 4 : 2, {out}))
     return vfail(GA_EINVAL, "logits and out must be aligned to their elements");
-  if (out == logits && (wide != in_f32 || (out_stride != logits_stride && rows > 1)))
-    return vfail(GA_EINVAL, "out may be logits only with its type and stride");
+  const int in_elt = in_f32 ? 4 : 2, out_elt = wide ? 4 : 2;
+  const bool in_place = out == logits && in_elt == out_elt && (out_stride == logits_stride || rows == 1);
+  if (!in_place && overlap({out, ((rows - 1LL) * out_stride + vocab) * out_elt},
+                           {logits, ((rows - 1LL) * logits_stride + vocab) * in_elt}))
+    return vfail(GA_EINVAL, "out overlaps logits; it may be logits itself with its type and stride");
   ga::LogitArgs a{};
   a.g = g;
   a.rules = *rules;

@@ -34,11 +34,13 @@ def _refused(call, good, bad, statuses):
 def test_page_table_errors():
     lib = G.load_library()
 
-    def call(lens=FAKE, S=5, spare=0, oo=FAKE, op=FAKE, So=3, nop=9, free=FAKE, nf=9, off=FAKE, pages=FAKE, cap=9):
+    def call(lens=FAKE, S=5, spare=0, oo=FAKE, op=FAKE, So=3, nop=9, free=FAKE, nf=9, off=FAKE + 512, pages=FAKE + 1024,
+             cap=9):
         return lib.graphattn_page_table(lens, S, spare, oo, op, So, nop, free, nf, off, pages, cap, None)
     bad = [dict(S=-1), dict(spare=-1), dict(nop=-1), dict(nf=-1), dict(cap=-1), dict(So=6), dict(So=-1), dict(lens=None),
            dict(oo=None), dict(op=None), dict(free=None), dict(off=None), dict(pages=None), dict(lens=ODD),
-           dict(off=FAKE + 4), dict(oo=FAKE + 4), dict(pages=ODD)]
+           dict(off=FAKE + 516), dict(oo=FAKE + 4), dict(pages=ODD), dict(pages=FAKE + 32), dict(off=FAKE + 16),
+           dict(pages=FAKE + 520)]
     _refused(call, {}, bad, [G.GA_EINVAL] * len(bad))
     assert call(nop=1 << 31) == G.GA_EUNSUPPORTED
 
@@ -58,9 +60,10 @@ BAD_GRAPHS = [dict(num_segments=-1), dict(num_branches=-1), dict(num_table_pages
 def test_slot_map_errors():
     lib = G.load_library()
 
-    def call(g=_graph(), counts=FAKE, off=FAKE, words=FAKE, pos=FAKE, branches=FAKE, cap=7):
+    def call(g=_graph(), counts=FAKE, off=FAKE + 512, words=FAKE + 1024, pos=FAKE + 2048, branches=FAKE + 4096, cap=7):
         return lib.graphattn_slot_map(ctypes.byref(g) if g else None, counts, off, words, pos, branches, cap, None)
-    bad = [dict(g=None), dict(off=None), dict(cap=-1), dict(off=ODD), dict(words=ODD), dict(counts=ODD)]
+    bad = [dict(g=None), dict(off=None), dict(cap=-1), dict(off=ODD), dict(words=ODD), dict(counts=ODD),
+           dict(words=FAKE), dict(pos=FAKE + 1048), dict(branches=FAKE + 520), dict(off=FAKE + 24)]
     bad += [dict(g=_graph(**x)) for x in BAD_GRAPHS]
     _refused(call, {}, bad, [G.GA_EINVAL] * len(bad))
     assert call(g=_graph(num_pages=(1 << 27) + 1)) == G.GA_EUNSUPPORTED
@@ -80,7 +83,7 @@ def test_qkv_append_errors():
                                         None)
     bad = [dict(pool=None), dict(q=None), dict(k=None), dict(v=None), dict(pos=None), dict(words=None), dict(out=None),
            dict(params=None), dict(transform=False), dict(n=-1), dict(qs=-8), dict(ks=9), dict(vs=4), dict(q=FAKE + 8),
-           dict(out=FAKE + 8), dict(pos=ODD), dict(out=FAKE), dict(t=dict(rotary_dim=-2)), dict(t=dict(rotary_dim=66)),
+           dict(out=FAKE + 8), dict(pos=ODD), dict(out=FAKE), dict(out=FAKE + 1024), dict(k=FAKE + 4112), dict(v=FAKE + 4096), dict(t=dict(rotary_dim=-2)), dict(t=dict(rotary_dim=66)),
            dict(t=dict(rotary_dim=31)), dict(t=dict(interleaved=2)), dict(t=dict(norm_eps=-1e-6)),
            dict(t=dict(norm_eps=float("nan"))), dict(t=dict(rotary_scale=float("inf"))), dict(t=dict(inv_freq=None)),
            dict(t=dict(inv_freq=FAKE + 4)), dict(t=dict(q_weight=FAKE + 4)), dict(t=dict(k_weight=FAKE + 8)),
@@ -106,7 +109,7 @@ def test_process_logits_errors():
            dict(r=dict(prompt_segments=-1)), dict(r=dict(num_bias=-1)), dict(r=dict(num_masks=-1)),
            dict(r=dict(mask_words=3)), dict(r=dict(masks=None)), dict(r=dict(row_mask=None)), dict(r=dict(bias_tokens=None)),
            dict(r=dict(bias_offsets=None)), dict(r=dict(bias_values=None)), dict(r=dict(repetition=ODD)),
-           dict(r=dict(bias_offsets=FAKE + 4)), dict(out=FAKE, so=200), dict(out=FAKE, dtype=G.GA_BF16, wide=1)]
+           dict(r=dict(bias_offsets=FAKE + 4)), dict(out=FAKE, so=200), dict(out=FAKE + 400), dict(out=FAKE, dtype=G.GA_BF16, wide=1)]
     bad += [dict(g=_graph(**x)) for x in BAD_GRAPHS]
     _refused(call, {}, bad, [G.GA_EINVAL] * len(bad))
     for change in (dict(dtype=G.GA_MXFP4), dict(dtype=7), dict(V=(1 << 28) + 1, si=1 << 31, so=1 << 31)):
