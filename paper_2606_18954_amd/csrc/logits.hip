@@ -322,7 +322,7 @@ __global__ __launch_bounds__(kThreads, 8) void k_logits(LogitArgs a) {
     if (flags) __syncthreads();
 
     const auto work = [&](const Values<TI, E>& in, int v, int m) {
-        unsigned allowed = ~0u;
+        unsigned allowed = 0;                        // (loaded ahead of the counts)
         if (row.mask) allowed = row.mask[v >> 5] >> (v & 31);
         float z[E];
 #pragma unroll
@@ -359,9 +359,11 @@ __global__ __launch_bounds__(kThreads, 8) void k_logits(LogitArgs a) {
             }
         }
 #pragma unroll
-        for (int k = 0; k < E; ++k) {
-          z[k] *= row.inv_t;
-          if (!((allowed >> k) & 1)) z[k] = -__builtin_inff();
+        for (int k = 0; k < E; ++k) z[k] *= row.inv_t;
+        if (row.mask) {
+#pragma unroll
+          for (int k = 0; k < E; ++k)
+            if (!((allowed >> k) & 1)) z[k] = -__builtin_inff();
         }
         if (m == E) {
           store<TO, E>(row.out, v, z);
