@@ -56,16 +56,19 @@ __device__ __forceinline__ int find(const int64_t* begin, int n, int64_t j) {
   return lo;
 }
 
-__device__ __forceinline__ int64_t held(const PageTableArgs& a, int64_t offset) {
-  return offset < 0 ? 0 : offset < a.n_old_pages ? offset : a.n_old_pages;
+// (fewer than 2^31 old pages: what is left of an offset fits 32 bits)
+__device__ __forceinline__ int32_t held(const PageTableArgs& a, int64_t offset) {
+  return offset < 0 ? 0 : (int32_t)(offset < a.n_old_pages ? offset : a.n_old_pages);
 }
 struct Need {
-  int64_t pages, had;
+  int32_t pages, had;
 };
-__device__ __forceinline__ Need need_of(const PageTableArgs& a, int32_t len, int64_t had) {
-  const int64_t want = ((int64_t)(len > 0 ? len : 0) + a.spare + kPageTokens - 1) / kPageTokens;
-  had = had < 0 ? 0 : had;
-  return {want > had ? want : had, had};
+__device__ __forceinline__ Need need_of(const PageTableArgs& a, int32_t len, int32_t had) {
+  len = max(len, 0);
+  had = max(had, 0);
+  // ceil((len + spare) / 16) without their sum, which may pass 32 bits.
+  const int32_t want = (len >> 4) + (a.spare >> 4) + (((len & 15) + (a.spare & 15) + kPageTokens - 1) >> 4);
+  return {max(want, had), had};
 }
 __device__ __forceinline__ Need need_of(const PageTableArgs& a, int32_t s) {
   return need_of(a, a.seg_len[s], s < a.S_old ? held(a, a.old_offsets[s + 1]) - held(a, a.old_offsets[s]) : 0);
@@ -88,7 +91,7 @@ __global__ __launch_bounds__(NT) void k_page_table(PageTableArgs a) {
     if (i < n) {
       const Need d = need_of(a, (int32_t)(t0 + i));
       begin[i] = d.pages;
-      had[i] = (int32_t)d.had;
+      had[i] = d.had;
       old[i] = t0 + i < a.S_old ? held(a, a.old_offsets[t0 + i]) : 0;
       mine.n += d.pages;
       mine.x += d.pages - d.had;
@@ -107,7 +110,7 @@ __global__ __launch_bounds__(NT) void k_page_table(PageTableArgs a) {
     const i32x4 len = *reinterpret_cast<const i32x4*>(a.seg_len + s);
     const i64x2 lo = *reinterpret_cast<const i64x2*>(a.old_offsets + s);
     const i64x2 hi = *reinterpret_cast<const i64x2*>(a.old_offsets + s + 2);
-    const int64_t o[5] = {held(a, lo[0]), held(a, lo[1]), held(a, hi[0]), held(a, hi[1]), held(a, a.old_offsets[s + 4])};
+    const int32_t o[5] = {held(a, lo[0]), held(a, lo[1]), held(a, hi[0]), held(a, hi[1]), held(a, a.old_offsets[s + 4])};
 #pragma unroll
     for (int k = 0; k < 4; ++k) add(need_of(a, len[k], o[k + 1] - o[k]));
   }
@@ -166,15 +169,15 @@ __global__ __launch_bounds__(NT) void k_slot_map(SlotMapArgs a) {
   int32_t* const token = reinterpret_cast<int32_t*>(base + a.tile);   // of its first row; may be below 0
   const int tid = threadIdx.x;
   const int32_t B = a.g.num_branches;
-  const int64_t t0 = (int64_t)blockIdx.x * a.tile;
-  const int n = (int)(B - t0 < a.tile ? B - t0 : a.tile);
+  const int64_t tile0 = (int64_t)blockIdx.x * a.tile;
+  const int n = (int)(B - tile0 < a.tile ? B - tile0 : a.tile);
   // Its branches' paths, by some lanes each.
   const int lane = tid % kGroup;
   for (int i0 = 0; i0 < n; i0 += NT / kGroup) {      // (whole waves go round, for the row operations)
     const int i = i0 + tid / kGroup;
     const bool there = i < n;
-    const int64_t c = there && a.counts ? count_of(a.counts[t0 + i]) : 1;
-    const PathRange p = there ? path_range(a.g, (int32_t)(t0 + i)) : PathRange{0, 0};
+    const int64_t c = there && a.counts ? count_of(a.counts[tile0 + i]) : 1;
+    const PathRange p = there ? path_range(a.g, (int32_t)(tile0 + i)) : PathRange{0, 0};
     int64_t before = 0;
     if (there && p.first >= p.end && lane == 0) {             // no segment: a token below 0 in every row
       token[i] = -0x7fffffff;
@@ -202,14 +205,14 @@ __global__ __launch_bounds__(NT) void k_slot_map(SlotMapArgs a) {
   }
   Two sum{0, 0}, before;
   if (a.counts) {
-    const int64_t whole = t0 & ~3LL;
+    const int64_t whole = tile0 & ~3LL;
 #pragma unroll 2
     for (int64_t b = 4 * tid; b < whole; b += 4 * NT) {
       const i32x4 c = *reinterpret_cast<const i32x4*>(a.counts + b);
 #pragma unroll
       for (int k = 0; k < 4; ++k) sum.n += count_of(c[k]);
     }
-    if (whole + tid < t0) sum.n += count_of(a.counts[whole + tid]);
+    if (whole + tid < tile0) sum.n += count_of(a.counts[whole + tid]);
   }
   __syncthreads();
   const int per = (a.tile + NT - 1) / NT;
@@ -217,14 +220,14 @@ __global__ __launch_bounds__(NT) void k_slot_map(SlotMapArgs a) {
   for (int k = 0; k < per; ++k)
     if (tid * per + k < n) mine.n += begin[tid * per + k];
   Two at = block_scan<NT>(mine, &total, sum, &before);
-  if (!a.counts) before = {t0, 0};
+  if (!a.counts) before = {tile0, 0};
   auto held = [](int64_t x) { return (int32_t)(x < 0x7fffffff ? x : 0x7fffffff); };
   for (int k = 0; k < per; ++k) {
     const int i = tid * per + k;
     if (i < n) {
       const int64_t c = begin[i];
       begin[i] = at.n;
-      if (blockIdx.y == 0) a.offsets[t0 + i] = held(before.n + at.n);
+      if (blockIdx.y == 0) a.offsets[tile0 + i] = held(before.n + at.n);
       at.n += c;
     }
   }
@@ -238,24 +241,37 @@ __global__ __launch_bounds__(NT) void k_slot_map(SlotMapArgs a) {
   for (int64_t j = 4 * ((int64_t)blockIdx.y * NT + tid); j < end; j += 4 * NT * (int64_t)gridDim.y) {
     i32x4 word, pos, branch;
     int i = n > 0 && j < rows ? find(begin, n, j) : 0;
-    int64_t entry = -1;                              // of the table, whose page `page` is
-    int32_t page = -1;
+    const int64_t next = i + 1 < n ? begin[i + 1] : total.n;
+    const int64_t t0 = n > 0 ? token[i] + (j - begin[i]) : -1;
+    if (j + 4 <= rows && j + 4 <= next && t0 >= 0 && (t0 & 15) <= 12 && base[i] + t0 < 0x7ffffff0LL) {
+      // Four tokens of one segment and page.
+      const int32_t page = a.words ? page_of(a.g, first[i], last[i], (int32_t)t0) : -1;
+      const int32_t w = page * kPageTokens + (int32_t)(t0 & (kPageTokens - 1)), p = (int32_t)(base[i] + t0);
+      const int32_t one = page < 0 ? 0 : 1, from = page < 0 ? -1 : w;
+      word = i32x4{from, from + one, from + 2 * one, from + 3 * one};
+      pos = i32x4{p, p + 1, p + 2, p + 3};
+      const int32_t b = (int32_t)tile0 + i;
+      branch = i32x4{b, b, b, b};
+    } else {
+      int64_t entry = -1;                            // of the table, whose page `page` is
+      int32_t page = -1;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      word[k] = pos[k] = branch[k] = -1;
-      if (j + k < rows) {
-        while (i + 1 < n && begin[i + 1] <= j + k) ++i;
-        const int64_t t = token[i] + (j + k - begin[i]), p = base[i] + t;
-        if (t >= 0 && p < 0x80000000LL) {
-          pos[k] = (int32_t)p;
-          branch[k] = (int32_t)t0 + i;
-          if (a.words) {
-            const int64_t at = first[i] + (t >> 4);
-            if (at != entry && at < last[i]) {
-              page = page_of(a.g, first[i], last[i], (int32_t)t);
-              entry = at;
+      for (int k = 0; k < 4; ++k) {
+        word[k] = pos[k] = branch[k] = -1;
+        if (j + k < rows) {
+          while (i + 1 < n && begin[i + 1] <= j + k) ++i;
+          const int64_t t = token[i] + (j + k - begin[i]), p = base[i] + t;
+          if (t >= 0 && p < 0x80000000LL) {
+            pos[k] = (int32_t)p;
+            branch[k] = (int32_t)tile0 + i;
+            if (a.words) {
+              const int64_t at = first[i] + (t >> 4);
+              if (at != entry && at < last[i]) {
+                page = page_of(a.g, first[i], last[i], (int32_t)t);
+                entry = at;
+              }
+              word[k] = at < last[i] && page >= 0 ? page * kPageTokens + (int32_t)(t & (kPageTokens - 1)) : -1;
             }
-            word[k] = at < last[i] && page >= 0 ? page * kPageTokens + (int32_t)(t & (kPageTokens - 1)) : -1;
           }
         }
       }
@@ -279,7 +295,7 @@ dim3 tiles_of(int64_t items, int64_t capacity, int threads, int32_t* tile) {
   const int64_t most = threads == 256 ? 512 : 256, t = (items + most - 1) / most;
   *tile = (int32_t)(t < 1 ? 1 : t > kMaxTile ? kMaxTile : t);
   const int64_t tiles = items > 0 ? (items + *tile - 1) / *tile : 1;
-  const int64_t want = capacity / (tiles * 4 * threads), room = 2048 * 256 / threads / tiles;
+  const int64_t want = capacity / (tiles * 4 * threads), room = 1024 * 256 / threads / tiles;
   const int64_t splits = want < room ? want : room;
   return dim3((unsigned)tiles, (unsigned)(splits < 1 ? 1 : splits));
 }
