@@ -7,10 +7,19 @@
 //
 // Counts are 16 bits a token of the slice: 14 bits of count, one for a token with a bias, one for a token of the
 // prompt (which counts for the repetition penalty alone).  Rows that could count further than 14 bits take the
-// slice in two halves with 32 bits a token.  Every workgroup of a row reads the whole path (4 bytes a token,
-// from L2: rows of one XCD are neighbours, whose paths share segments).
-// Biases: the flag says that there is one, and its value is looked up (the row's list is ascending).
-// Memory bounds it: a row of V values of four bytes moves 8 V.
+// slice in two halves with 32 bits a token.  Every workgroup of a row reads the whole path (4 bytes a token, four
+// tokens a load, from L2: rows of one XCD are neighbours, whose paths share segments).
+// Biases: the flag says that there is one.  A list of up to 512 a row lies in LDS with the place of the first bias of
+// every 32 tokens; a longer one is searched in memory.
+//
+// Memory bounds it: 1024 rows of 152064 float32 values with penalties and biases, 1.25 GB in 250-257 us (a plain copy:
+// 234; without rules 238).  Eight waves per SIMD hide the counting (55 registers; at five 376 us): what is uniform and
+// rare, counts of 32 bits, has a loop of its own.  1024 rows of four drafted tokens a branch, 65024 bf16 values to
+// float32, contexts of some 14000 tokens: 100 us, where the same without penalties takes 63 and a copy 69: the vector
+// unit is busy two thirds of the time, with counting a quarter of it.  128 rows of 50001 with 300 biases and a mask each:
+// 14 us, half of it the chain from the branch to its tokens' counts; one row 6.2.
+// (Rows of a branch in one workgroup that goes on with their counts: the drafts 115 us where they took 122, but the 1024
+// rows 303 where they took 256.  Values of 8 bytes a load where the output is twice as wide: 84 -> 63 us without rules.)
 #include <type_traits>
 
 #include "pool_load.hpp"
@@ -155,7 +164,8 @@ __device__ __forceinline__ void store(unsigned char* row, int v, const float (&z
 
 template <class TI, class TO>
 __global__ __launch_bounds__(kThreads, 8) void k_logits(LogitArgs a) {
-  constexpr int E = 16 / sizeof(TO), LOADS = sizeof(TI) == 4 ? 3 : 16 / E;  // values of a load; loads of a thread in flight together
+  // Values of a load; loads of a thread in flight together.
+  constexpr int E = 16 / sizeof(TO), LOADS = sizeof(TI) == 4 ? 3 : 16 / E;
   extern __shared__ unsigned counts[];
   __shared__ Path path;
   __shared__ int64_t said_of, tokens_of;
@@ -209,7 +219,8 @@ __global__ __launch_bounds__(kThreads, 8) void k_logits(LogitArgs a) {
   const bool flags = a.counted || biased;
   const auto clear = [&]() {
     typedef unsigned u32x4_lds __attribute__((ext_vector_type(4), aligned(16)));
-    for (int i = tid; i < a.slice / 8 + 4; i += kThreads) reinterpret_cast<u32x4_lds*>(counts)[i] = u32x4_lds{0, 0, 0, 0};
+    for (int i = tid; i < a.slice / 8 + 4; i += kThreads)
+      reinterpret_cast<u32x4_lds*>(counts)[i] = u32x4_lds{0, 0, 0, 0};
   };
   if (flags) clear();
   PathRange range{0, 0};
@@ -322,56 +333,56 @@ __global__ __launch_bounds__(kThreads, 8) void k_logits(LogitArgs a) {
     if (flags) __syncthreads();
 
     const auto work = [&](const Values<TI, E>& in, int v, int m) {
-        unsigned allowed = 0;                        // (loaded ahead of the counts)
-        if (row.mask) allowed = row.mask[v >> 5] >> (v & 31);
-        float z[E];
+      unsigned allowed = 0;                        // (loaded ahead of the counts)
+      if (row.mask) allowed = row.mask[v >> 5] >> (v & 31);
+      float z[E];
 #pragma unroll
-        for (int k = 0; k < E; ++k) z[k] = in.at(k);
-        if (flags) {
-          constexpr int W = WIDE ? E : E / 2;
-          const unsigned* const word = counts + (WIDE ? v - lo : (v - lo) >> 1);
-          unsigned w[W], any = 0;
+      for (int k = 0; k < E; ++k) z[k] = in.at(k);
+      if (flags) {
+        constexpr int W = WIDE ? E : E / 2;
+        const unsigned* const word = counts + (WIDE ? v - lo : (v - lo) >> 1);
+        unsigned w[W], any = 0;
 #pragma unroll
-          for (int k = 0; k < W; ++k) any |= w[k] = word[k];
-          // The tokens that have a bias, one after the other: few have.
-          if (any & (WIDE ? 0x40000000u : 0x40004000u)) {
-            unsigned some = 0;
+        for (int k = 0; k < W; ++k) any |= w[k] = word[k];
+        // The tokens that have a bias, one after the other: few have.
+        if (any & (WIDE ? 0x40000000u : 0x40004000u)) {
+          unsigned some = 0;
 #pragma unroll
-            for (int k = 0; k < E; ++k)
-              some |= w[WIDE ? k : k / 2] & (WIDE ? 0x40000000u : k & 1 ? 0x40000000u : 0x4000u) ? 1u << k : 0u;
-            for (some &= (1u << m) - 1; some; some &= some - 1) {
-              const int j = __builtin_ctz(some);
-              const float bias =
-                  near ? sum_from(near_list, near_first[(v + j - lo) >> 5], n_bias, v + j)
-                       : sum_of(a.rules.bias_tokens + bias_first, a.rules.bias_values + bias_first, n_bias, v + j);
+          for (int k = 0; k < E; ++k)
+            some |= w[WIDE ? k : k / 2] & (WIDE ? 0x40000000u : k & 1 ? 0x40000000u : 0x4000u) ? 1u << k : 0u;
+          for (some &= (1u << m) - 1; some; some &= some - 1) {
+            const int j = __builtin_ctz(some);
+            const float bias =
+                near ? sum_from(near_list, near_first[(v + j - lo) >> 5], n_bias, v + j)
+                     : sum_of(a.rules.bias_tokens + bias_first, a.rules.bias_values + bias_first, n_bias, v + j);
 #pragma unroll
-              for (int k = 0; k < E; ++k) z[k] += j == k ? bias : 0.f;
-            }
+            for (int k = 0; k < E; ++k) z[k] = j == k ? z[k] + bias : z[k];
           }
-          if (any && a.counted)
-#pragma unroll
-            for (int k = 0; k < E; ++k) {
-              const unsigned u = WIDE ? w[k] : k & 1 ? w[k / 2] >> 16 : w[k / 2] & 0xffffu;
-              const unsigned count = u & (WIDE ? 0x3fffffffu : 0x3fffu);
-              const float size = z[k] > 0.f ? row.inv_rep : row.rep;
-              if (u & (WIDE ? 0xbfffffffu : 0xbfffu)) z[k] *= size;
-              if (count) z[k] -= row.freq * (float)count + row.pres;
-            }
         }
+        if (any && a.counted)
 #pragma unroll
-        for (int k = 0; k < E; ++k) z[k] *= row.inv_t;
-        if (row.mask) {
+          for (int k = 0; k < E; ++k) {
+            const unsigned u = WIDE ? w[k] : k & 1 ? w[k / 2] >> 16 : w[k / 2] & 0xffffu;
+            const unsigned count = u & (WIDE ? 0x3fffffffu : 0x3fffu);
+            const float size = z[k] > 0.f ? row.inv_rep : row.rep;
+            if (u & (WIDE ? 0xbfffffffu : 0xbfffu)) z[k] *= size;
+            if (count) z[k] -= row.freq * (float)count + row.pres;
+          }
+      }
 #pragma unroll
-          for (int k = 0; k < E; ++k)
-            if (!((allowed >> k) & 1)) z[k] = -__builtin_inff();
-        }
-        if (m == E) {
-          store<TO, E>(row.out, v, z);
-        } else {
+      for (int k = 0; k < E; ++k) z[k] *= row.inv_t;
+      if (row.mask) {
 #pragma unroll
-          for (int k = 0; k < E; ++k)
-            if (k < m) reinterpret_cast<TO*>(row.out)[v + k] = (TO)z[k];
-        }
+        for (int k = 0; k < E; ++k)
+          if (!((allowed >> k) & 1)) z[k] = -__builtin_inff();
+      }
+      if (m == E) {
+        store<TO, E>(row.out, v, z);
+      } else {
+#pragma unroll
+        for (int k = 0; k < E; ++k)
+          if (k < m) reinterpret_cast<TO*>(row.out)[v + k] = (TO)z[k];
+      }
     };
     if constexpr (WIDE) {
       // (rare: one load at a time)
@@ -402,7 +413,8 @@ __global__ __launch_bounds__(kThreads, 8) void k_logits(LogitArgs a) {
 
 hipError_t launch_logits(const LogitArgs& args, bool in_f32, bool out_f32, hipStream_t stream) {
   LogitArgs a = args;
-  // Slices of a row: as many as its counts need, and so many that a few rows fill the device.
+  // Slices of a row: as many as its counts need, and so many that a few rows fill the device.  (128 rows of 50001: 512
+  // workgroups 14.6 us, 1024 20.0; one row is as fast in 8, 16 or 32.)
   const bool biased = a.rules.bias_offsets != nullptr;
   const int64_t largest = biased ? kMaxSliceBiased : kMaxSlice;
   const int64_t least = (a.vocab + largest - 1) / largest, most = (a.vocab + 2047) / 2048;

@@ -6,11 +6,18 @@
 // channel c with partner c' is rs (x[c] w[c] C[c] + x[c'] w[c'] S[c]): the weights are folded into C and S once
 // for all heads of a token, and a head costs two products a channel and the sum of its squares.
 //
-// A wave takes a token and some groups of its heads; 8 channels a lane, 16 bytes of bf16, so D / 8 lanes hold a
-// head and 512 / D heads are a group.  The token's rotary_dim / 2 angles are the lanes', one each (float64 product
-// and remainder in turns, then sine and cosine of half turns in float32); the lanes fetch those of their channels
-// from each other.  No table of angles is read, and positions may be any int32.  The next group's loads go out
-// before the present one is worked on.
+// 8 channels a lane, 16 bytes of bf16, so D / 8 lanes hold a head and a wave's load is a group of 512 / D heads.  A
+// workgroup takes one token, or four where there are many.  A token's rotary_dim / 2 angles are a wave's lanes', one
+// each (float64 product and remainder in turns, then sine and cosine of half turns in float32); they and the weights go
+// through LDS.  No table of angles is read, and positions may be any int32.  The groups are dealt to the waves in
+// units, three of q or one of k with the same heads of v, so that all loads of a unit go out before its first store:
+// a wave that waits for a load behind a store waits for the store too.
+//
+// Memory bounds it: 32768 tokens of 40 + 2 x 8 heads of 128, bf16, 940 MB in 186 us = 5.05 TB/s (a plain copy of as
+// many bytes runs at 5.3), without norms or rotation 185; of 28 + 2 x 4 heads 105 us = 5.76 TB/s; a step's 1024 tokens
+// 5.5 us, one token 3.1 (replayed from a graph).  Counters: reads and writes are what the rows hold, the vector unit is
+// busy 37% of the time.  Before: one group after the other with a load ahead, angles exchanged between lanes and made
+// by every wave, 226 us and 20; five groups of q a unit 192 and 6.9 (more registers, five waves per SIMD).
 #include "mxfp4.hpp"
 #include "pool_load.hpp"
 #include "step_internal.hpp"
@@ -21,6 +28,7 @@ namespace {
 constexpr int kWaves = 4;          // of a workgroup
 
 // Groups of heads that a wave takes at once, all of their loads ahead of the first store: of q, or of k and of v.
+// (Two to five of q, one or two of k and v: 185 to 192 us for the 32768 tokens above; float32 two or three: the same.)
 template <class T>
 struct Units {
   static constexpr int Q = sizeof(T) == 4 ? 2 : 3, KV = 1;
@@ -82,8 +90,8 @@ __device__ __forceinline__ float head_sum(float s) {
   return s;
 }
 
-// What the heads of a kind are made with: cosine and sine of this lane's channels (the sine with its sign), weights folded
-// in, and where the partners are.
+// What the heads of a kind are made with: cosine and sine of this lane's channels (the sine with its sign), weights
+// folded in.
 struct Turn {
   float c[8], s[8];
   bool normed;
@@ -265,16 +273,19 @@ void launch(const QkvArgs& a, dim3 grid, int dtype, bool pairs, hipStream_t stre
 hipError_t launch_qkv(const QkvArgs& args, int dim, int dtype, bool interleaved, hipStream_t stream) {
   QkvArgs a = args;
   const int group = 512 / dim, nq = (a.Hq + group - 1) / group, nk = (a.Hkv + group - 1) / group;
-  const int q = dtype == GA_F32 ? Units<float>::Q : Units<__bf16>::Q, kv = dtype == GA_F32 ? Units<float>::KV : Units<__bf16>::KV;
+  const int q = dtype == GA_F32 ? Units<float>::Q : Units<__bf16>::Q;
+  const int kv = dtype == GA_F32 ? Units<float>::KV : Units<__bf16>::KV;
   a.q_units = (nq + q - 1) / q;
   a.q_groups = (nq + a.q_units - 1) / a.q_units;
-  // What is written goes past the caches where they could not hold it for the attention that follows.
+  // What is written goes past the caches where they could not hold it for the attention that follows (186 us, not 191,
+  // for the 940 MB above); a step's rows stay.
   a.past = (int64_t)a.n * (a.Hq + 2 * a.Hkv) * dim * (dtype == GA_F32 ? 4 : 2) > (32 << 20);
-  // Four tokens a workgroup where there are enough of them to fill the device, else one, its units on as many
-  // workgroups as they need.
+  // Four tokens a workgroup where there are enough of them to fill the device (one: 207 us, two: 193, four: 192 before
+  // the other steps), else one, its units on as many workgroups as they need.
   a.tokens = a.n >= 4096 ? kWaves : 1;
   const int units = a.q_units + (nk + kv - 1) / kv;
-  const dim3 grid((unsigned)((a.n + a.tokens - 1) / a.tokens), (unsigned)(a.tokens > 1 ? 1 : (units + kWaves - 1) / kWaves));
+  const dim3 grid((unsigned)((a.n + a.tokens - 1) / a.tokens),
+                  (unsigned)(a.tokens > 1 ? 1 : (units + kWaves - 1) / kWaves));
   if (dim == 64) launch<64>(a, grid, dtype, interleaved, stream);
   else launch<128>(a, grid, dtype, interleaved, stream);
   return hipGetLastError();
