@@ -8,11 +8,11 @@
 // Counts are 16 bits a token of the slice: 14 bits of count, one for a token with a bias, one for a token of the
 // prompt (which counts for the repetition penalty alone).  Rows that could count further than 14 bits take the
 // slice in two halves with 32 bits a token.  Every workgroup of a row reads the whole path (4 bytes a token, four
-// tokens a load, from L2: rows of one XCD are neighbours, whose paths share segments).
+// tokens a load, from L2).
 // Biases: the flag says that there is one.  A list of up to 512 a row lies in LDS with the place of the first bias of
 // every 32 tokens; a longer one is searched in memory.
 //
-// Memory bounds it: 1024 rows of 152064 float32 values with penalties and biases, 1.25 GB in 250-257 us (a plain copy:
+// Memory bounds it: 1024 rows of 152064 float32 values with penalties and biases, 1.25 GB in 248-254 us (a plain copy:
 // 234; without rules 238).  Eight waves per SIMD hide the counting (55 registers; at five 376 us): what is uniform and
 // rare, counts of 32 bits, has a loop of its own.  1024 rows of four drafted tokens a branch, 65024 bf16 values to
 // float32, contexts of some 14000 tokens: 100 us, where the same without penalties takes 63 and a copy 69: the vector
@@ -171,10 +171,9 @@ __global__ __launch_bounds__(kThreads, 8) void k_logits(LogitArgs a) {
   __shared__ int64_t said_of, tokens_of;
   __shared__ int32_t fours_of;
   const int tid = threadIdx.x;
-  // Workgroups go round the 8 XCDs: a row's stay on one, with its neighbours'.
-  const int64_t q = blockIdx.x / 8;
-  const int64_t r = (int64_t)(blockIdx.x % 8) * a.rows_per_xcd + q / a.parts;
-  if (q / a.parts >= a.rows_per_xcd || r >= a.rows) return;
+  // (A row's workgroups go round the XCDs.  Kept on one, with their neighbours', the path's tokens would come from one
+  // L2, but a row of 152064 alone would have an eighth of the device: 10.4 us, not 6.1; 1024 rows 253, not 248.)
+  const int64_t q = blockIdx.x, r = q / a.parts;
   const int lo0 = (int)(q % a.parts) * a.slice, hi0 = min(lo0 + a.slice, a.vocab);
   const int32_t b = a.row_branches ? a.row_branches[r] : (int32_t)r;
   if (b < 0 || b >= a.g.num_branches) return;
@@ -422,8 +421,7 @@ hipError_t launch_logits(const LogitArgs& args, bool in_f32, bool out_f32, hipSt
   parts = parts < least ? least : parts > most ? most : parts;
   a.slice = (int32_t)(((a.vocab + parts - 1) / parts + 31) / 32 * 32);
   a.parts = (a.vocab + a.slice - 1) / a.slice;
-  a.rows_per_xcd = (a.rows + 7) / 8;
-  const int64_t grid = (int64_t)a.rows_per_xcd * 8 * a.parts;
+  const int64_t grid = (int64_t)a.rows * a.parts;
   if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
   const size_t lds = (size_t)a.slice * 2 + 64 + (biased ? kBias * 8 + a.slice / 16 : 0);
   const dim3 g((unsigned)grid), t(kThreads);

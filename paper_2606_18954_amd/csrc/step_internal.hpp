@@ -58,7 +58,6 @@ struct LogitArgs {
   const int32_t* row_positions;
   int32_t rows, vocab;
   int32_t slice, parts;          // tokens of a workgroup (a multiple of 32), workgroups of a row
-  int32_t rows_per_xcd;
   bool counted;                  // repetition, frequency or presence
 };
 

@@ -535,13 +535,15 @@ def page_table(seg_len, free_pages, spare: int = 0, old_offsets=None, old_pages=
 def slot_map(graph: DeviceGraph, counts=None, token_offsets=None, slot_words=None, positions=None, branches=None,
              capacity=None, stream=None):
     """graphattn_slot_map: (token_offsets int32 [B + 1], slot_words, positions, branches int32 [capacity]) of every
-    branch's newest counts[b] tokens (one each without counts).  Where an output is given, it has the capacity; else
-    `capacity` (one row a branch without it)."""
+    branch's newest counts[b] tokens (one each without counts).  The rows are those of the outputs that are given, else
+    `capacity`, which only a call without counts knows by itself: one a branch."""
     torch = _torch or _load_torch()
     lib = load_library()
     B, given = graph.num_branches, [t for t in (slot_words, positions, branches) if t is not None]
     device = graph.tensors[0].device
     handle = _stream_handle(stream, graph.tensors[0])
+    if counts is not None and capacity is None and not given:
+        raise ValueError("capacity: how many rows the counts may add up to")
     n = min(int(t.numel()) for t in given) if given else B if capacity is None else int(capacity)
     if capacity is not None and n < capacity:
         raise ValueError("slot_words, positions and branches must be int32 [capacity], contiguous")

@@ -533,3 +533,31 @@ def test_two_calls_at_once():
         U.check_logits(x.c, host(x.out_buffer), x.before)
     for c in (p, q):
         U.check_slots(c, *run_slots(c))
+
+
+def test_captured_rules_of_large_slices():
+    """Slices whose counts fill half of a CU's LDS, captured and replayed over new logits and positions."""
+    require_gpu()
+    rng = np.random.default_rng(47)
+    g = U.random_graph(rng, 12)
+    c = U.logits_case(rng, g, 520, 38001, "f32", rules="rfpt")
+    s = Logits(c)
+    s.call()
+    captured = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(captured):
+        s.call()
+    for i in range(3):
+        c["logits"] = U.stored(rng.standard_normal(c["logits"].shape), "f32")
+        c["positions"] = rng.integers(-1, 100, 520).astype(np.int32)
+        s.buffer.copy_(dev(c["logits"]))
+        s.positions.copy_(dev(c["positions"]))
+        s.out_buffer.fill_(9.0)
+        captured.replay()
+        torch.cuda.synchronize()
+        got = s.out_buffer.clone()
+        s.out_buffer.fill_(9.0)
+        assert torch.equal(s.call(), got), i
+    keep = rng.permutation(520)[:40]
+    for k in ("logits", "branches", "positions", "rep", "freq", "pres", "temp"):
+        c[k] = c[k][keep]
+    U.check_logits(c, host(got)[keep], np.full((40, 38001), 9, np.float32))

@@ -178,6 +178,19 @@ def test_page_table_refusals():
         G.page_table(i32(3), i32(9))
 
 
+def test_slot_map_refusals(graph, monkeypatch):
+    monkeypatch.setattr(G, "_stream_handle", lambda *a: 0)       # (no device here)
+    with pytest.raises(ValueError, match="capacity"):
+        G.slot_map(graph, i32(2))
+    with pytest.raises(ValueError, match="int32"):
+        G.slot_map(graph, None, None, i32(3), capacity=4)
+    for change, match in ((dict(counts=i64(2)), "counts"), (dict(counts=i32(1)), "counts")):
+        with pytest.raises(ValueError, match=match):
+            G.slot_map(graph, **change, capacity=4)
+    with pytest.raises(ValueError, match="GPU"):
+        G.slot_map(graph)
+
+
 def test_transform_refusals():
     f64, f32 = torch.zeros(32, dtype=torch.float64), torch.zeros(64)
     with pytest.raises(ValueError, match="inv_freq"):
