@@ -22,7 +22,8 @@ extern "C" {
 
 /* A rollout graph in device memory: ga_segment_table and ga_branch_paths (graphattn.h) with the same meaning
  * and the extents of their arrays.  A length below 0 counts as 0, a segment id outside [0, num_segments) as an
- * empty segment, and a page-table entry outside its segment's, or a page id outside [0, num_pages), as no page. */
+ * empty segment, a path whose offsets decrease or start outside path_segs as empty, and a page-table entry outside
+ * its segment's or the table's, or a page id outside [0, num_pages), as no page. */
 typedef struct {
   int32_t num_segments;
   int32_t num_branches;
@@ -69,8 +70,8 @@ ga_status graphattn_page_table(const int32_t* seg_len, int32_t num_segments, int
  *   branches      [capacity] device int32: b
  * Rows from the total to capacity are padding, as are the tokens of a branch without a path, whose last segment
  * is outside the graph, with t < 0 or with a position of 2^31 or more: slot word, position and branch are -1.
- * Rows from capacity on are not written.  slot_words, positions and branches may each be NULL; GA_EINVAL where an output
- * overlaps another array.  Branches that
+ * Rows from capacity on are not written.  slot_words, positions and branches may each be NULL; GA_EINVAL where an
+ * output overlaps another array.  Branches that
  * end in the same segment name the same slots (graphattn_kv_append wants them once). */
 ga_status graphattn_slot_map(const ga_device_graph* graph, const int32_t* new_counts,
                              int32_t* token_offsets, int32_t* slot_words, int32_t* positions,

@@ -101,7 +101,7 @@ template <int D, class T, bool FP4, bool PAIRS>
 __global__ __launch_bounds__(64 * kWaves) void k_qkv(QkvArgs a) {
   constexpr int LPH = D / 8, HPG = 64 / LPH, SZ = (int)sizeof(T), ROW = D * SZ;
   using U = Units<T>;
-  __shared__ __align__(16) float cosines[kWaves][64], sines[kWaves][64], weights[2 * D];
+  __shared__ __align__(16) float cosines[kWaves][64], sines[kWaves][64], weights[2 * D + 8];   // (and eight zeros)
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int64_t first = (int64_t)blockIdx.x * a.tokens;
@@ -125,6 +125,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_qkv(QkvArgs a) {
   }
   for (int i = threadIdx.x; i < 2 * D; i += 64 * kWaves)
     if (const float* const w = i < D ? a.weight[0] : a.weight[1]) weights[i] = w[i & (D - 1)];
+  if (threadIdx.x < 8) weights[2 * D + threadIdx.x] = 0.f;
   if (wave < a.tokens && lane < half) {
     const int32_t pos = first + wave < a.n ? a.positions[first + wave] : 0;
     const double t = (double)pos * (a.inv_freq[lane] * 0.15915494309189533577);
@@ -157,10 +158,12 @@ __global__ __launch_bounds__(64 * kWaves) void k_qkv(QkvArgs a) {
     t->normed = normed;
     if (normed) {
       const float* const w = weights + kind * D;
+      const float* const partners = turns ? w + pc : weights + 2 * D;
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         t->c[k] *= w[c + k];
-        t->s[k] *= w[PAIRS ? c + (k ^ 1) : pc + k];
+        if constexpr (PAIRS) t->s[k] *= c + k < 2 * half ? w[c + (k ^ 1)] : 0.f;
+        else t->s[k] *= partners[k];
       }
     }
   };

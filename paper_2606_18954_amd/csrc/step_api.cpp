@@ -177,7 +177,8 @@ ga_status graphattn_qkv_append(void* kv_page_pool, const void* q, const void* k,
   if (overlap({out}, {{q, in_place ? 0 : ((n - 1) * q_stride + q_row) * elt},
                       {k, ((n - 1) * k_stride + kv_row) * elt},
                       {v, ((n - 1) * v_stride + kv_row) * elt}}))
-    return vfail(GA_EINVAL, "q_out overlaps the rows that are read; it may be q itself where q's rows lie one behind the other");
+    return vfail(GA_EINVAL,
+                 "q_out overlaps the rows that are read; it may be q itself where q's rows lie one behind the other");
   ga::QkvArgs a{};
   a.src[0] = static_cast<const unsigned char*>(q);
   a.src[1] = static_cast<const unsigned char*>(k);

@@ -99,7 +99,8 @@ __device__ __forceinline__ PathRange path_range(const ga_device_graph& g, int32_
   return {first, e < g.num_path_segs ? e : g.num_path_segs};
 }
 
-// Sums over a wave by row operations (a scan through lane exchanges waits for LDS twelve times, a microsecond): CTRL's lane, or nothing where a row or a mask leaves it out, is added.
+// Sums over a wave by row operations (a scan through lane exchanges waits for LDS twelve times, a microsecond):
+// CTRL's lane, or nothing where a row or a mask leaves it out, is added.
 template <int CTRL, int ROWS>
 __device__ __forceinline__ void add_lane(int64_t* v) {
   const int lo = __builtin_amdgcn_update_dpp(0, (int)*v, CTRL, ROWS, 0xf, false);

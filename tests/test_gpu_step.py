@@ -561,3 +561,18 @@ def test_captured_rules_of_large_slices():
     for k in ("logits", "branches", "positions", "rep", "freq", "pres", "temp"):
         c[k] = c[k][keep]
     U.check_logits(c, host(got)[keep], np.full((40, 38001), 9, np.float32))
+
+
+def test_a_weight_stays_with_its_channel():
+    """An infinite weight of a channel that does not turn reaches no other and is not multiplied by an angle."""
+    require_gpu()
+    rng = np.random.default_rng(48)
+    for inter in (False, True):
+        c = U.qkv_case(rng, 3, 2, 1, 64, "f32", 16, inter)
+        c["positions"][:] = [0, 7, 900]
+        c["weights"][0][40] = np.inf
+        out = host(Qkv(c).call())
+        assert np.isposinf(np.abs(out[:, :, 40])).all()
+        c["weights"][0][40] = 0
+        out[:, :, 40] = 0
+        U.check_rows(out, U.qkv_parts(c)[0], c, c["weights"][0], np.ones(3, dtype=bool))
