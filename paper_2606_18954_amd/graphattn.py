@@ -602,8 +602,8 @@ def qkv_append(pool, q, k, v, positions, slot_words, transform: QKTransform, par
     pool's slots.  q, k and v may be parts of one projection's rows (strided tokens); positions and slot_words int32
     [n]: a position below 0 is padding, a word outside the pool stores nothing."""
     torch = _torch or _load_torch()
-    lib = load_library()
-    n, Hq, Hkv, D = int(positions.numel()), params.num_q_heads, params.num_kv_heads, params.head_dim
+    lib = _lib or load_library()
+    n, Hq, Hkv, D = positions.numel(), params.num_q_heads, params.num_kv_heads, params.head_dim
     layout = _layout(params, n)
     handle = _enter(stream, pool, layout)
     row = layout[2] if layout else q.dtype
@@ -611,15 +611,18 @@ def qkv_append(pool, q, k, v, positions, slot_words, transform: QKTransform, par
         raise ValueError(f"a transform of {transform.head_dim}-wide heads for {D}-wide ones")
     if q_out is None:
         q_out = torch.zeros((n, Hq, D), dtype=row, device=q.device)
-    what = "positions and slot_words must be int32, one per token"
-    pw, ww = _array(positions, torch.int32, n, what), _array(slot_words, torch.int32, n, what)
+    if positions.dtype != torch.int32 or slot_words.dtype != torch.int32 or slot_words.numel() < n:
+        raise ValueError("positions and slot_words must be int32, one per token")
+    if q_out.dtype != row or q_out.numel() < n * Hq * D:
+        raise ValueError("q_out must be [tokens, Hq, D] of q's type, contiguous")
     shape = (n, Hkv, D)
     qp, qs = _rows(q, (n, Hq, D), row)
     kp, ks = _rows(k, shape, row)
     vp, vs = _rows(v, shape, row)
-    op = _array(q_out, row, n * Hq * D, "q_out must be [tokens, Hq, D] of q's type, contiguous")
-    _check(lib.graphattn_qkv_append(_dev_ptr(pool), qp, kp, vp, qs, ks, vs, pw, ww, n, op, transform.ref,
-                                    ctypes.byref(params), handle))
+    status = lib.graphattn_qkv_append(_dev_ptr(pool), qp, kp, vp, qs, ks, vs, _dev_ptr(positions), _dev_ptr(slot_words), n,
+                                      _dev_ptr(q_out), transform.ref, ctypes.byref(params), handle)
+    if status:
+        _check(status)
     return q_out
 
 
