@@ -130,7 +130,7 @@ typedef struct {
 } ga_logit_rules;
 
 /* Logits of a step's rows put through these rules, in this order for row r and token v, in float32:
- *   z = logits[r][v] + bias;  repetition;  z - (f count + presence [count > 0]);  z / temperature;
+ *   z = logits[r][v] + bias;  repetition;  z - f count - presence where count > 0;  z / temperature;
  *   -infinity where the row's mask forbids v (whatever z is, NaN too);  rounded to out's type.
  * The context of row r is the tokens of its branch's path up to and with its position (slot_map's positions and
  * branches; a row that checks a drafted token sees those before it): token t of a segment in slot w is

@@ -361,19 +361,22 @@ __global__ __launch_bounds__(kThreads, 8) void k_logits(LogitArgs a) {
         if (any && a.counted)
 #pragma unroll
           for (int k = 0; k < E; ++k) {
-            const unsigned u = WIDE ? w[k] : k & 1 ? w[k / 2] >> 16 : w[k / 2] & 0xffffu;
-            const unsigned count = u & (WIDE ? 0x3fffffffu : 0x3fffu);
+            const unsigned u = w[WIDE ? k : k / 2];
+            const float count = (float)(WIDE ? u & 0x3fffffffu : (u >> (16 * (k & 1))) & 0x3fffu);
             const float size = z[k] > 0.f ? row.inv_rep : row.rep;
-            if (u & (WIDE ? 0xbfffffffu : 0xbfffu)) z[k] *= size;
-            if (count) z[k] -= row.freq * (float)count + row.pres;
+            if (u & (WIDE ? 0xbfffffffu : 0xbfffu << (16 * (k & 1)))) z[k] *= size;
+            // (not as products with 0: an infinite penalty bans what came and nothing else)
+            if (count > 0.f) z[k] = __builtin_fmaf(-row.freq, count, z[k]) - row.pres;
           }
       }
 #pragma unroll
       for (int k = 0; k < E; ++k) z[k] *= row.inv_t;
       if (row.mask) {
 #pragma unroll
-        for (int k = 0; k < E; ++k)
-          if (!((allowed >> k) & 1)) z[k] = -__builtin_inff();
+        for (int k = 0; k < E; ++k) {
+          const unsigned keep = (unsigned)((int)(allowed << (31 - k)) >> 31);
+          z[k] = __builtin_bit_cast(float, (__builtin_bit_cast(unsigned, z[k]) & keep) | (0xff800000u & ~keep));
+        }
       }
       if (m == E) {
         store<TO, E>(row.out, v, z);

@@ -576,3 +576,20 @@ def test_a_weight_stays_with_its_channel():
         c["weights"][0][40] = 0
         out[:, :, 40] = 0
         U.check_rows(out, U.qkv_parts(c)[0], c, c["weights"][0], np.ones(3, dtype=bool))
+
+
+def test_an_infinite_penalty_bans_what_came_and_nothing_else():
+    require_gpu()
+    rng = np.random.default_rng(49)
+    g = U.graph([30, 10], [[0, 1], [0]], rng)
+    for name in ("freq", "pres", "rep"):
+        c = U.logits_case(rng, g, 2, 300, "f32", rules="rfp", drafts=False, prompt=0)
+        c["ids"][:] = rng.integers(0, 40, len(c["ids"]))
+        c["logits"] = -np.abs(c["logits"]) - 1
+        c["rep"][:], c["freq"][:], c["pres"][:] = 1, 0, 0
+        c[name][:] = np.inf
+        out = host(Logits(c).call())
+        for r in range(2):
+            came = {v for v, _ in S.context(U.oracle_graph(g), r, None, c["ids"], 0)}
+            gone = np.isin(np.arange(300), list(came))
+            assert (out[r, gone] == -np.inf).all() and (out[r, ~gone] == c["logits"][r, ~gone]).all(), name
