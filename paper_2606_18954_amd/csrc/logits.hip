@@ -12,10 +12,10 @@
 // Biases: the flag says that there is one.  A list of up to 512 a row lies in LDS with the place of the first bias of
 // every 32 tokens; a longer one is searched in memory.
 //
-// Memory bounds it: 1024 rows of 152064 float32 values with penalties and biases, 1.25 GB in 244-254 us (a plain copy:
+// Memory bounds it: 1024 rows of 152064 float32 values with penalties and biases, 1.25 GB in 238-254 us (a plain copy:
 // 234; without rules 238).  Eight waves per SIMD hide the counting (55 registers; at five 376 us): what is uniform and
 // rare, counts of 32 bits, has a loop of its own.  1024 rows of four drafted tokens a branch, 65024 bf16 values to
-// float32, contexts of some 14000 tokens: 100 us, where the same without penalties takes 63 and a copy 69: the
+// float32, contexts of some 14000 tokens: 96 us, where the same without penalties takes 63 and a copy 69: the
 // vector unit is busy two thirds of the time.  128 rows of 50001 with 300 biases and a mask each: 14 us, half of it the
 // chain from the branch to its tokens' counts; one row 6.2.
 // (Rows of a branch in one workgroup that goes on with their counts: the drafts 115 us where they took 122, but the
