@@ -13,11 +13,12 @@
 // units, three of q or one of k with the same heads of v, so that all loads of a unit go out before its first store:
 // a wave that waits for a load behind a store waits for the store too.
 //
-// Memory bounds it: 32768 tokens of 40 + 2 x 8 heads of 128, bf16, 940 MB in 170-187 us = 5.0-5.5 TB/s (a plain copy of as
-// many bytes runs at 5.3), without norms or rotation 185; of 28 + 2 x 4 heads 105 us = 5.76 TB/s; a step's 1024 tokens
-// 5.5 us, one token 3.1 (replayed from a graph).  Counters: reads and writes are what the rows hold, the vector unit is
-// busy 37% of the time.  Before: one group after the other with a load ahead, angles exchanged between lanes and made
-// by every wave, 226 us and 20; five groups of q a unit 192 and 6.9 (more registers, five waves per SIMD).
+// Memory bounds it: 32768 tokens of 40 + 2 x 8 heads of 128, bf16, 940 MB in 170-187 us = 5.0-5.5 TB/s by the card (a
+// plain copy of as many bytes runs at 5.3), without norms or rotation the same; of 28 + 2 x 4 heads 105 us = 5.76 TB/s;
+// a step's 1024 tokens 5.5 us, one token 3.1 (replayed from a graph).  Counters: reads and writes are what the rows
+// hold, the vector unit is busy 37% of the time.  Before: one group after the other with a load ahead, angles exchanged
+// between lanes and made by every wave, 226 us and 20; five groups of q a unit 192 and 6.9 (more registers, five waves
+// per SIMD).
 #include "mxfp4.hpp"
 #include "pool_load.hpp"
 #include "step_internal.hpp"
