@@ -50,7 +50,10 @@ typedef struct {
  * free_pages [num_free]: device; num_old_segments in [0, num_segments], 0 for a table that starts (old_offsets
  * and old_pages may be NULL).  old_offsets holds what an earlier call wrote (or any CSR from 0 on); a value outside
  * [0, num_old_pages] is taken as the nearer end.  GA_EINVAL where an output overlaps
- * another array. */
+ * another array.
+ * Every call, and every replay of a captured one, takes from the front of the list as it then is: before the
+ * next one the caller drops the entries that were taken, total less sum of old of them, from free_pages, or the
+ * same pages go to two segments.  An old page of -1 stays -1. */
 ga_status graphattn_page_table(const int32_t* seg_len, int32_t num_segments, int32_t spare_tokens,
                                const int64_t* old_offsets, const int32_t* old_pages,
                                int32_t num_old_segments, int64_t num_old_pages,

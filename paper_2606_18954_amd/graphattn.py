@@ -510,7 +510,9 @@ def page_table(seg_len, free_pages, spare: int = 0, old_offsets=None, old_pages=
                stream=None):
     """graphattn_page_table: (seg_page_offsets int64 [S + 1], seg_pages int32) on the device.  Every segment keeps its
     pages of the old table (its first len(old_offsets) - 1 segments) and gets more from the front of free_pages, for
-    seg_len + spare tokens.  Without `pages` a tensor of all old and free pages' size is made, -1 behind the table."""
+    seg_len + spare tokens.  Without `pages` a tensor of all old and free pages' size is made, -1 behind the table.
+    The next call's old_pages are its first total = seg_page_offsets[-1] entries, and its free_pages those behind the
+    total - (old total) that this one took: nothing else marks them as taken."""
     torch = _torch or _load_torch()
     lib = load_library()
     S, known = int(seg_len.numel()), 0 if old_offsets is None else int(old_offsets.numel()) - 1
