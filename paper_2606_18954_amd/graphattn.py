@@ -7,10 +7,12 @@ the process has no GPU, the compute entry points raise instead of falling back t
 Tensors are contiguous and on one device.  The calls that take a pool check the element types of the pool,
 of the rows beside it and of slot words, lse and masses, and that each holds what the call reads or writes
 (about a microsecond a call); ValueError otherwise.  Without a stream a call goes to the current stream of
-the current device, and a pool (or mass) of another device is refused.
+the current device, and a pool (or mass) of another device is refused.  Outputs that a call makes itself are
+made on the stream that it goes to.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
 import os
@@ -261,6 +263,17 @@ def _stream_handle(stream, t=None) -> int:
     return int(_raw_stream(device))
 
 
+def _on(stream):
+    """Where a call makes its own outputs: on its stream.  On another one a fill could run after the call, and memory
+    could be taken that earlier work there still uses."""
+    if stream is None:
+        return contextlib.nullcontext()
+    torch = _torch or _load_torch()
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream.cuda_stream))
+    return torch.cuda.stream(stream)
+
+
 def _dev_ptr(t) -> int:
     if t is None:
         return 0
@@ -346,9 +359,11 @@ def decode(q, pool, graph: HostGraph, params: Params, out=None, lse=None, stream
     B = graph.bp.num_branches
     if out is None:
         odt = torch.float32 if params.out_f32 else q.dtype
-        out = torch.empty((B, params.num_q_heads, params.head_dim), dtype=odt, device=q.device)
+        with _on(stream):
+            out = torch.empty((B, params.num_q_heads, params.head_dim), dtype=odt, device=q.device)
     if lse is None:
-        lse = torch.empty((B, params.num_q_heads), dtype=torch.float32, device=q.device)
+        with _on(stream):
+            lse = torch.empty((B, params.num_q_heads), dtype=torch.float32, device=q.device)
     handle = _enter(stream, pool, _layout(params, B), q)
     _check_rows(_row_sizes(params, B), q, out, lse)
     _check(lib.graphattn_decode(_dev_ptr(q), _dev_ptr(pool), ctypes.byref(graph.st),
@@ -385,9 +400,11 @@ def extend(q, pool, graph: HostGraph, query_counts, params: Params, out=None, ls
     R = int(cnt.sum())
     if out is None:
         odt = torch.float32 if params.out_f32 else q.dtype
-        out = torch.empty((R, params.num_q_heads, params.head_dim), dtype=odt, device=q.device)
+        with _on(stream):
+            out = torch.empty((R, params.num_q_heads, params.head_dim), dtype=odt, device=q.device)
     if lse is None:
-        lse = torch.empty((R, params.num_q_heads), dtype=torch.float32, device=q.device)
+        with _on(stream):
+            lse = torch.empty((R, params.num_q_heads), dtype=torch.float32, device=q.device)
     handle = _enter(stream, pool, _layout(params, R), q)
     _check_rows(_row_sizes(params, R), q, out, lse)
     _check(lib.graphattn_extend(_dev_ptr(q), _dev_ptr(pool), ctypes.byref(graph.st),
@@ -432,9 +449,11 @@ def kv_read(pool, slot_words, params: Params, k_out=None, v_out=None, stream=Non
     shape = (n, params.num_kv_heads, params.head_dim)
     dt = torch.float32 if params.dtype == GA_F32 else torch.bfloat16
     if k_out is None:
-        k_out = torch.zeros(shape, dtype=dt, device=pool.device)
+        with _on(stream):
+            k_out = torch.zeros(shape, dtype=dt, device=pool.device)
     if v_out is None:
-        v_out = torch.zeros(shape, dtype=dt, device=pool.device)
+        with _on(stream):
+            v_out = torch.zeros(shape, dtype=dt, device=pool.device)
     if k_out.shape != shape or v_out.shape != shape:
         raise ValueError("one K row and one V row [Hkv, D] per slot word")
     if k_out.dtype != dt or v_out.dtype != dt or slot_words.dtype != torch.int32:
@@ -521,9 +540,11 @@ def page_table(seg_len, free_pages, spare: int = 0, old_offsets=None, old_pages=
         raise ValueError("old_offsets [segments + 1] and old_pages come together")
     handle = _stream_handle(stream, seg_len) if seg_len.is_cuda else 0
     if offsets is None:
-        offsets = torch.empty(S + 1, dtype=torch.int64, device=seg_len.device)
+        with _on(stream):
+            offsets = torch.empty(S + 1, dtype=torch.int64, device=seg_len.device)
     if pages is None:
-        pages = torch.full((had + int(free_pages.numel()),), -1, dtype=torch.int32, device=seg_len.device)
+        with _on(stream):
+            pages = torch.full((had + int(free_pages.numel()),), -1, dtype=torch.int32, device=seg_len.device)
     _check(lib.graphattn_page_table(
         _array(seg_len, torch.int32, S, "seg_len must be int32, contiguous"), S, int(spare),
         _array(old_offsets, torch.int64, 0, "old_offsets must be int64, contiguous"),
@@ -550,9 +571,11 @@ def slot_map(graph: DeviceGraph, counts=None, token_offsets=None, slot_words=Non
     if capacity is not None and n < capacity:
         raise ValueError("slot_words, positions and branches must be int32 [capacity], contiguous")
     if not given:
-        slot_words, positions, branches = (torch.empty(n, dtype=torch.int32, device=device) for _ in range(3))
+        with _on(stream):
+            slot_words, positions, branches = (torch.empty(n, dtype=torch.int32, device=device) for _ in range(3))
     if token_offsets is None:
-        token_offsets = torch.empty(B + 1, dtype=torch.int32, device=device)
+        with _on(stream):
+            token_offsets = torch.empty(B + 1, dtype=torch.int32, device=device)
     what = "slot_words, positions and branches must be int32 [capacity], contiguous"
     _check(lib.graphattn_slot_map(
         graph.ref, _array(counts, torch.int32, B, "counts must be int32 [branches], contiguous"),
@@ -612,7 +635,8 @@ def qkv_append(pool, q, k, v, positions, slot_words, transform: QKTransform, par
     if transform.head_dim != D:
         raise ValueError(f"a transform of {transform.head_dim}-wide heads for {D}-wide ones")
     if q_out is None:
-        q_out = torch.zeros((n, Hq, D), dtype=row, device=q.device)
+        with _on(stream):
+            q_out = torch.zeros((n, Hq, D), dtype=row, device=q.device)
     if positions.dtype != torch.int32 or slot_words.dtype != torch.int32 or slot_words.numel() < n:
         raise ValueError("positions and slot_words must be int32, one per token")
     if q_out.dtype != row or q_out.numel() < n * Hq * D:
@@ -682,7 +706,8 @@ def process_logits(logits, rules: LogitRules, graph: Optional[DeviceGraph] = Non
     rows, vocab = logits.shape
     handle = _stream_handle(stream, logits) if logits.is_cuda else 0
     if out is None:
-        out = torch.zeros((rows, vocab), dtype=torch.float32 if out_f32 else logits.dtype, device=logits.device)
+        with _on(stream):
+            out = torch.zeros((rows, vocab), dtype=torch.float32 if out_f32 else logits.dtype, device=logits.device)
     if out.shape != logits.shape or out.dtype not in (torch.float32, logits.dtype):
         raise ValueError("out must be [rows, vocab], float32 or of the logits' type")
     if rules.rows is not None and rules.rows < rows:
@@ -723,7 +748,8 @@ def equivalence_classes(z, forest: HostForest, kappa: float, labels=None, stream
     if z.dim() != 2 or z.shape[0] != N:
         raise ValueError("one embedding row per state")
     if labels is None:
-        labels = torch.empty(N, dtype=torch.int32, device=z.device)
+        with _on(stream):
+            labels = torch.empty(N, dtype=torch.int32, device=z.device)
     _check(lib.graphattn_equivalence_classes(_dev_ptr(z), int(z.shape[1]),
                                              GA_BF16 if z.dtype == torch.bfloat16 else GA_F32,
                                              ctypes.byref(forest.c), float(kappa),
@@ -738,15 +764,17 @@ def graph_suffix(labels, forest: HostForest, capacity=None, stream=None):
     lib = load_library()
     N = forest.c.num_states
     total = ctypes.c_int64(0)
-    offs = torch.empty(N + 1, dtype=torch.int64, device=labels.device)
     cap = int(capacity) if capacity is not None else 0
-    states = torch.empty(max(cap, 1), dtype=torch.int32, device=labels.device)
+    with _on(stream):
+        offs = torch.empty(N + 1, dtype=torch.int64, device=labels.device)
+        states = torch.empty(max(cap, 1), dtype=torch.int32, device=labels.device)
     st = lib.graphattn_graph_suffix(_dev_ptr(labels), ctypes.byref(forest.c), _dev_ptr(offs),
                                     _dev_ptr(states), cap, ctypes.byref(total),
                                     _stream_handle(stream))
     if st == GA_ERANGE and capacity is None:
         cap = int(total.value)
-        states = torch.empty(max(cap, 1), dtype=torch.int32, device=labels.device)
+        with _on(stream):
+            states = torch.empty(max(cap, 1), dtype=torch.int32, device=labels.device)
         st = lib.graphattn_graph_suffix(_dev_ptr(labels), ctypes.byref(forest.c), _dev_ptr(offs),
                                         _dev_ptr(states), cap, ctypes.byref(total),
                                         _stream_handle(stream))
@@ -770,7 +798,8 @@ class Forest:
         import torch
         N = self.host.c.num_states
         if labels is None:
-            labels = torch.empty(N, dtype=torch.int32, device=z.device)
+            with _on(stream):
+                labels = torch.empty(N, dtype=torch.int32, device=z.device)
         _check(self.lib.graphattn_forest_classes(
             self.handle, _dev_ptr(z), int(z.shape[1]),
             GA_BF16 if z.dtype == torch.bfloat16 else GA_F32, float(kappa), _dev_ptr(labels),
@@ -784,8 +813,9 @@ class Forest:
         import torch
         N = self.host.c.num_states
         if out is None:
-            out = {k: torch.empty(N, dtype=torch.float64, device=labels.device)
-                   for k in ("score", "step_reward", "a_cor", "a_eff", "a_dual")}
+            with _on(stream):
+                out = {k: torch.empty(N, dtype=torch.float64, device=labels.device)
+                       for k in ("score", "step_reward", "a_cor", "a_eff", "a_dual")}
         adv = Advantages(*[_dev_ptr(out[k]) for k in ("score", "step_reward", "a_cor", "a_eff",
                                                       "a_dual")])
         _check(self.lib.graphattn_forest_advantages(
@@ -976,9 +1006,11 @@ class Evict:
         if mass.numel() < 16 * self.num_pages or mass.dtype != torch.float32:
             raise ValueError("one mass per slot of the pool, float32")
         if positions is None:
-            positions = torch.empty(self.total, dtype=torch.int32, device=mass.device)
+            with _on(stream):
+                positions = torch.empty(self.total, dtype=torch.int32, device=mass.device)
         if slot_words is None:
-            slot_words = torch.empty(self.total, dtype=torch.int32, device=mass.device)
+            with _on(stream):
+                slot_words = torch.empty(self.total, dtype=torch.int32, device=mass.device)
         if positions.numel() < self.total or slot_words.numel() < self.total:
             raise ValueError("one position and one slot word per token that stays")
         if positions.dtype != torch.int32 or slot_words.dtype != torch.int32:
