@@ -86,7 +86,8 @@ ga_status graphattn_slot_map(const ga_device_graph* graph, const int32_t* new_co
  * (i, i + rotary_dim / 2), or (2i, 2i + 1) where interleaved, becomes
  *   (a cos - b sin, b cos + a sin) * rotary_scale,    angle p * inv_freq[i]
  * (p * inv_freq[i] and its remainder in float64, sine and cosine float32).  Values are float32 throughout and
- * are rounded once, at the end. */
+ * are rounded once, at the end; a norm holds for all finite x, those too whose squares leave float32's range (a head of
+ * zeros with a norm_eps of 0 is NaN). */
 typedef struct {
   int32_t rotary_dim;      /* 0 .. D, even; a multiple of 16 unless interleaved (GA_EUNSUPPORTED otherwise) */
   int32_t interleaved;     /* 0 or 1 */

@@ -190,7 +190,22 @@ __global__ __launch_bounds__(64 * kWaves) void k_qkv(QkvArgs a) {
       float s = 0.f;
 #pragma unroll
       for (int k = 0; k < 8; ++k) s += x[k] * x[k];
-      const float rs = __builtin_amdgcn_rsqf(head_sum<D>(s) * (1.f / D) + a.eps);
+      float mean = head_sum<D>(s) * (1.f / D) + a.eps;
+      // Squares that leave float32's range (or are subnormal, which the root takes as 0): the heads that have them
+      // once more, their values times a power of two.
+      const bool low = mean < 0x1p-100f, leaves = low || !(mean < __builtin_inff());
+      if (__any(leaves)) {
+        const float by = !leaves ? 1.f : low ? 0x1p96f : 0x1p-96f;
+        s = 0.f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          x[k] *= by;
+          z[k] = x[k] * t.c[k] + p[k] * by * t.s[k];
+          s += x[k] * x[k];
+        }
+        mean = head_sum<D>(s) * (1.f / D) + a.eps * by * by;
+      }
+      const float rs = __builtin_amdgcn_rsqf(mean);
 #pragma unroll
       for (int k = 0; k < 8; ++k) z[k] *= rs;
     }
