@@ -107,7 +107,7 @@ typedef struct {
  *                 (its query is written: a token that is in the pool already)
  *   q_out         [n][Hq][D] device, 16-byte aligned; may be q itself where q_stride = Hq D
  * Slot words of tokens that are stored must be distinct.  Only params->num_q_heads, num_kv_heads, head_dim,
- * dtype and num_pages are used.  num_tokens 0: nothing is launched. */
+ * dtype and num_pages are used.  num_tokens 0: nothing is launched; more than 2^26 - 4: GA_EUNSUPPORTED. */
 ga_status graphattn_qkv_append(void* kv_page_pool, const void* q, const void* k, const void* v,
                                int64_t q_stride, int64_t k_stride, int64_t v_stride,
                                const int32_t* positions, const int32_t* slot_words, int32_t num_tokens,
@@ -149,7 +149,8 @@ typedef struct {
  *   token_ids     [num_pages x 16] device int32, one per slot of the pool
  * Where neither repetition, frequency nor presence is given the context is not read, and graph and token_ids may
  * be NULL (row_branches and row_positions mark padding all the same).  A mask that forbids everything leaves a row
- * of -infinity.  Of a context the first 2^31 - 1 tokens
+ * of -infinity.  GA_EUNSUPPORTED where rows x ceil(vocab / 38912) is 2^22 or more (with biases: vocab / 36864), and
+ * for a vocab above 2^28.  Of a context the first 2^31 - 1 tokens
  * are seen, and a token's count is exact up to 2^30 - 1. */
 ga_status graphattn_process_logits(const void* logits, int64_t logits_stride, int32_t rows,
                                    int32_t vocab, int32_t dtype, const ga_logit_rules* rules,

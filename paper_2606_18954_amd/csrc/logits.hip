@@ -413,21 +413,21 @@ __global__ __launch_bounds__(kThreads, 8) void k_logits(LogitArgs a) {
 
 }  // namespace
 
-hipError_t launch_logits(const LogitArgs& args, bool in_f32, bool out_f32, hipStream_t stream) {
-  LogitArgs a = args;
+int64_t plan_logits(LogitArgs* a) {
   // Slices of a row: as many as its counts need, and so many that a few rows fill the device.  (128 rows of 50001: 512
   // workgroups 14.6 us, 1024 20.0; one row is as fast in 8, 16 or 32.)
-  const bool biased = a.rules.bias_offsets != nullptr;
-  const int64_t largest = biased ? kMaxSliceBiased : kMaxSlice;
-  const int64_t least = (a.vocab + largest - 1) / largest, most = (a.vocab + 2047) / 2048;
-  int64_t parts = (512 + a.rows - 1) / a.rows;
+  const int64_t largest = a->rules.bias_offsets ? kMaxSliceBiased : kMaxSlice;
+  const int64_t least = (a->vocab + largest - 1) / largest, most = (a->vocab + 2047) / 2048;
+  int64_t parts = (512 + a->rows - 1) / a->rows;
   parts = parts < least ? least : parts > most ? most : parts;
-  a.slice = (int32_t)(((a.vocab + parts - 1) / parts + 31) / 32 * 32);
-  a.parts = (a.vocab + a.slice - 1) / a.slice;
-  const int64_t grid = (int64_t)a.rows * a.parts;
-  if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
-  const size_t lds = (size_t)a.slice * 2 + 64 + (biased ? kBias * 8 + a.slice / 16 : 0);
-  const dim3 g((unsigned)grid), t(kThreads);
+  a->slice = (int32_t)(((a->vocab + parts - 1) / parts + 31) / 32 * 32);
+  a->parts = (a->vocab + a->slice - 1) / a->slice;
+  return (int64_t)a->rows * a->parts * kThreads;
+}
+
+hipError_t launch_logits(const LogitArgs& a, bool in_f32, bool out_f32, hipStream_t stream) {
+  const size_t lds = (size_t)a.slice * 2 + 64 + (a.rules.bias_offsets ? kBias * 8 + a.slice / 16 : 0);
+  const dim3 g((unsigned)(a.rows * a.parts)), t(kThreads);
   if (in_f32) hipLaunchKernelGGL((k_logits<float, float>), g, t, lds, stream, a);
   else if (out_f32) hipLaunchKernelGGL((k_logits<__bf16, float>), g, t, lds, stream, a);
   else hipLaunchKernelGGL((k_logits<__bf16, __bf16>), g, t, lds, stream, a);

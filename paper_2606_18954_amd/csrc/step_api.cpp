@@ -158,7 +158,9 @@ ga_status graphattn_qkv_append(void* kv_page_pool, const void* q, const void* k,
   if (misaligned(8, {transform->inv_freq}) || misaligned(16, {transform->q_weight, transform->k_weight}))
     return vfail(GA_EINVAL, "inv_freq must be 8-byte aligned, the weights 16-byte aligned");
   if (num_tokens < 0) return vfail(GA_EINVAL, "num_tokens is negative");
-  if (num_tokens > (1 << 28)) return vfail(GA_EUNSUPPORTED, "%d tokens (> 2^28)", num_tokens);
+  // (256 threads for four tokens)
+  if ((num_tokens + 3LL) / 4 * 256 >= ga::kLaunchThreads)
+    return vfail(GA_EUNSUPPORTED, "%d tokens (> 2^26 - 4)", num_tokens);
   if (params->num_q_heads > (1 << 14)) return vfail(GA_EUNSUPPORTED, "%d heads (> 2^14)", params->num_q_heads);
   if (num_tokens == 0) return GA_OK;
   if (!kv_page_pool || !q || !k || !v || !positions || !slot_words || !q_out)
@@ -262,6 +264,8 @@ ga_status graphattn_process_logits(const void* logits, int64_t logits_stride, in
   a.rows = rows;
   a.vocab = vocab;
   a.counted = counted;
+  if (ga::plan_logits(&a) >= ga::kLaunchThreads)
+    return vfail(GA_EUNSUPPORTED, "%d rows of %d: %d parts a row are 2^22 or more in all", rows, vocab, a.parts);
   const hipError_t e = ga::launch_logits(a, in_f32, wide, static_cast<hipStream_t>(hip_stream));
   return e == hipSuccess ? GA_OK : ga::host_hip_fail(e, "logits launch");
 }

@@ -61,9 +61,14 @@ struct LogitArgs {
   bool counted;                  // repetition, frequency or presence
 };
 
+// A launch has fewer threads along x.
+constexpr int64_t kLaunchThreads = 1LL << 32;
+
 hipError_t launch_page_table(const PageTableArgs& a, hipStream_t stream);
 hipError_t launch_slot_map(const SlotMapArgs& a, hipStream_t stream);
 hipError_t launch_qkv(const QkvArgs& a, int dim, int dtype, bool interleaved, hipStream_t stream);
+// Slices of the rows, into a; the threads of the launch.
+int64_t plan_logits(LogitArgs* a);
 hipError_t launch_logits(const LogitArgs& a, bool in_f32, bool out_f32, hipStream_t stream);
 
 namespace {
