@@ -7,7 +7,8 @@ the process has no GPU, the compute entry points raise instead of falling back t
 Tensors are contiguous and on one device.  The calls that take a pool check the element types of the pool,
 of the rows beside it and of slot words, lse and masses, and that each holds what the call reads or writes
 (about a microsecond a call); ValueError otherwise.  Without a stream a call goes to the current stream of
-the current device, and a pool (or mass) of another device is refused.  Outputs that a call makes itself are
+the current device, and a pool (or mass) of another device is refused; the calls between two attention calls
+refuse tensors of two devices.  Outputs that a call makes itself are
 made on the stream that it goes to.
 """
 from __future__ import annotations
@@ -274,11 +275,20 @@ def _on(stream):
     return torch.cuda.stream(stream)
 
 
-def _dev_ptr(t) -> int:
+def _elsewhere(at: int, device):
+    """Refuses a tensor of device `at` (-1: the host) beside others of `device`.  (Callers look first: a call of one small
+    kernel costs ten microseconds, and has up to ten tensors.)"""
+    if at < 0:
+        raise ValueError("tensors passed to the library must live on the GPU")
+    raise ValueError(f"tensors of one call live on one device, not on {device} and {at}")
+
+
+def _dev_ptr(t, device=None) -> int:
     if t is None:
         return 0
-    if not t.is_cuda:
-        raise ValueError("tensors passed to the library must live on the GPU")
+    at = t.get_device()
+    if at < 0 or (device is not None and at != device):
+        _elsewhere(at, device)
     if not t.is_contiguous():
         raise ValueError("tensors passed to the library must be contiguous")
     return int(t.data_ptr())
@@ -484,14 +494,21 @@ def empty_pool(params: Params, device="cuda"):
     return torch.empty((n, h, 2, 16, d), dtype=dt, device=device)
 
 
-def _array(t, dtype, n: int, what: str) -> int:
-    """Pointer of a contiguous device tensor of this type with n elements at least (0 for None); `what` says so."""
+def _device(tensors):
+    """The device of the first of some tensors that may be None; None where all are."""
+    return next((t.get_device() for t in tensors if t is not None), None)
+
+
+def _array(t, dtype, n: int, what: str, device=None) -> int:
+    """Pointer of a contiguous tensor of this type, on this device, with n elements at least (0 for None); `what` says
+    so."""
     if t is None:
         return 0
     if t.dtype != dtype or t.numel() < n or not t.is_contiguous():
         raise ValueError(what)
-    if not t.is_cuda:
-        raise ValueError("tensors passed to the library must live on the GPU")
+    at = t.get_device()
+    if at < 0 or (device is not None and at != device):
+        _elsewhere(at, device)
     return t.data_ptr()
 
 
@@ -499,6 +516,8 @@ class DeviceGraph:
     """ga_device_graph: a rollout graph's index arrays as torch tensors on the device (kept, not copied: what a
     call reads is what they hold when it runs).  seg_len int32 [S], seg_page_offsets int64 [S + 1], seg_pages
     int32, path_offsets int64 [B + 1], path_segs int32; num_pages: of the pool."""
+
+    device = None                                      # of its tensors
 
     def __init__(self, seg_len, seg_page_offsets, seg_pages, path_offsets, path_segs, num_pages: int):
         torch = _torch or _load_torch()
@@ -508,13 +527,14 @@ class DeviceGraph:
         if self.num_branches < 0:
             raise ValueError("path_offsets must be int64 [branches + 1]")
         S = self.num_segments
+        d = self.device = seg_len.get_device()
         self.c = DeviceGraphC(
             S, self.num_branches, int(seg_pages.numel()), int(path_segs.numel()), self.num_pages,
-            _array(seg_len, torch.int32, S, "seg_len must be int32, contiguous"),
-            _array(seg_page_offsets, torch.int64, S + 1, "seg_page_offsets must be int64 [segments + 1], contiguous"),
-            _array(seg_pages, torch.int32, 0, "seg_pages must be int32, contiguous"),
-            _array(path_offsets, torch.int64, 1, "path_offsets must be int64 [branches + 1], contiguous"),
-            _array(path_segs, torch.int32, 0, "path_segs must be int32, contiguous"))
+            _array(seg_len, torch.int32, S, "seg_len must be int32, contiguous", d),
+            _array(seg_page_offsets, torch.int64, S + 1, "seg_page_offsets must be int64 [segments + 1], contiguous", d),
+            _array(seg_pages, torch.int32, 0, "seg_pages must be int32, contiguous", d),
+            _array(path_offsets, torch.int64, 1, "path_offsets must be int64 [branches + 1], contiguous", d),
+            _array(path_segs, torch.int32, 0, "path_segs must be int32, contiguous", d))
         self.ref = ctypes.byref(self.c)
 
     @classmethod
@@ -538,7 +558,7 @@ def page_table(seg_len, free_pages, spare: int = 0, old_offsets=None, old_pages=
     had = 0 if old_pages is None else int(old_pages.numel())
     if known < 0 or (known > 0) > (old_pages is not None):
         raise ValueError("old_offsets [segments + 1] and old_pages come together")
-    handle = _stream_handle(stream, seg_len) if seg_len.is_cuda else 0
+    handle, d = _stream_handle(stream, seg_len) if seg_len.is_cuda else 0, seg_len.get_device()
     if offsets is None:
         with _on(stream):
             offsets = torch.empty(S + 1, dtype=torch.int64, device=seg_len.device)
@@ -547,11 +567,11 @@ def page_table(seg_len, free_pages, spare: int = 0, old_offsets=None, old_pages=
             pages = torch.full((had + int(free_pages.numel()),), -1, dtype=torch.int32, device=seg_len.device)
     _check(lib.graphattn_page_table(
         _array(seg_len, torch.int32, S, "seg_len must be int32, contiguous"), S, int(spare),
-        _array(old_offsets, torch.int64, 0, "old_offsets must be int64, contiguous"),
-        _array(old_pages, torch.int32, 0, "old_pages must be int32, contiguous"), known, had,
-        _array(free_pages, torch.int32, 0, "free_pages must be int32, contiguous"), int(free_pages.numel()),
-        _array(offsets, torch.int64, S + 1, "offsets must be int64 [segments + 1], contiguous"),
-        _array(pages, torch.int32, 0, "pages must be int32, contiguous"), int(pages.numel()), handle))
+        _array(old_offsets, torch.int64, 0, "old_offsets must be int64, contiguous", d),
+        _array(old_pages, torch.int32, 0, "old_pages must be int32, contiguous", d), known, had,
+        _array(free_pages, torch.int32, 0, "free_pages must be int32, contiguous", d), int(free_pages.numel()),
+        _array(offsets, torch.int64, S + 1, "offsets must be int64 [segments + 1], contiguous", d),
+        _array(pages, torch.int32, 0, "pages must be int32, contiguous", d), int(pages.numel()), handle))
     return offsets, pages
 
 
@@ -563,7 +583,7 @@ def slot_map(graph: DeviceGraph, counts=None, token_offsets=None, slot_words=Non
     torch = _torch or _load_torch()
     lib = load_library()
     B, given = graph.num_branches, [t for t in (slot_words, positions, branches) if t is not None]
-    device = graph.tensors[0].device
+    device, d = graph.tensors[0].device, graph.tensors[0].get_device()
     handle = _stream_handle(stream, graph.tensors[0])
     if counts is not None and capacity is None and not given:
         raise ValueError("capacity: how many rows the counts may add up to")
@@ -578,10 +598,10 @@ def slot_map(graph: DeviceGraph, counts=None, token_offsets=None, slot_words=Non
             token_offsets = torch.empty(B + 1, dtype=torch.int32, device=device)
     what = "slot_words, positions and branches must be int32 [capacity], contiguous"
     _check(lib.graphattn_slot_map(
-        graph.ref, _array(counts, torch.int32, B, "counts must be int32 [branches], contiguous"),
-        _array(token_offsets, torch.int32, B + 1, "token_offsets must be int32 [branches + 1], contiguous"),
-        _array(slot_words, torch.int32, n, what), _array(positions, torch.int32, n, what),
-        _array(branches, torch.int32, n, what), n, handle))
+        graph.ref, _array(counts, torch.int32, B, "counts must be int32 [branches], contiguous", d),
+        _array(token_offsets, torch.int32, B + 1, "token_offsets must be int32 [branches + 1], contiguous", d),
+        _array(slot_words, torch.int32, n, what, d), _array(positions, torch.int32, n, what, d),
+        _array(branches, torch.int32, n, what, d), n, handle))
     return token_offsets, slot_words, positions, branches
 
 
@@ -599,15 +619,16 @@ class QKTransform:
         if not scale:
             raise ValueError("scale must not be 0")
         self.head_dim, self.tensors = int(head_dim), (inv_freq, q_norm, k_norm)
+        d = self.device = _device(self.tensors)
         what = "q_norm and k_norm must be float32 [head_dim], contiguous"
         self.c = QKTransformC(rotary, int(bool(interleaved)), float(eps), float(scale),
-                              _array(inv_freq, torch.float64, 0, "inv_freq must be float64, contiguous"),
-                              _array(q_norm, torch.float32, head_dim, what),
-                              _array(k_norm, torch.float32, head_dim, what))
+                              _array(inv_freq, torch.float64, 0, "inv_freq must be float64, contiguous", d),
+                              _array(q_norm, torch.float32, head_dim, what, d),
+                              _array(k_norm, torch.float32, head_dim, what, d))
         self.ref = ctypes.byref(self.c)
 
 
-def _rows(t, shape: tuple, dtype) -> tuple:
+def _rows(t, shape: tuple, dtype, device=None) -> tuple:
     """(pointer, values from a token's heads to the next one's) of rows [n, heads, dim]; the heads of a token lie one
     behind the other."""
     if t.dtype != dtype or t.shape != shape:
@@ -616,8 +637,9 @@ def _rows(t, shape: tuple, dtype) -> tuple:
     token, head, channel = t.stride()
     if (channel != 1 or (heads > 1 and head != dim)) and n:
         raise ValueError("the heads of a token must lie one behind the other")
-    if not t.is_cuda:
-        raise ValueError("tensors passed to the library must live on the GPU")
+    at = t.get_device()
+    if at < 0 or (device is not None and at != device):
+        _elsewhere(at, device)
     return t.data_ptr(), token if n > 1 else heads * dim
 
 
@@ -641,12 +663,15 @@ def qkv_append(pool, q, k, v, positions, slot_words, transform: QKTransform, par
         raise ValueError("positions and slot_words must be int32, one per token")
     if q_out.dtype != row or q_out.numel() < n * Hq * D:
         raise ValueError("q_out must be [tokens, Hq, D] of q's type, contiguous")
-    shape = (n, Hkv, D)
+    shape, d = (n, Hkv, D), q.get_device()
+    if transform.device is not None and transform.device != d:
+        raise ValueError(f"the transform's tensors live on device {transform.device}, q on {d}")
     qp, qs = _rows(q, (n, Hq, D), row)
-    kp, ks = _rows(k, shape, row)
-    vp, vs = _rows(v, shape, row)
-    status = lib.graphattn_qkv_append(_dev_ptr(pool), qp, kp, vp, qs, ks, vs, _dev_ptr(positions), _dev_ptr(slot_words), n,
-                                      _dev_ptr(q_out), transform.ref, ctypes.byref(params), handle)
+    kp, ks = _rows(k, shape, row, d)
+    vp, vs = _rows(v, shape, row, d)
+    status = lib.graphattn_qkv_append(_dev_ptr(pool, d), qp, kp, vp, qs, ks, vs, _dev_ptr(positions, d),
+                                      _dev_ptr(slot_words, d), n, _dev_ptr(q_out, d), transform.ref, ctypes.byref(params),
+                                      handle)
     if status:
         _check(status)
     return q_out
@@ -658,11 +683,14 @@ class LogitRules:
     set bit: the token may come) with row_mask int32 [rows] (outside [0, masks): none).  None leaves a rule out; the
     first prompt_segments of a path count for the repetition penalty alone."""
 
+    device = None                                      # of its tensors
+
     def __init__(self, repetition=None, frequency=None, presence=None, temperature=None, prompt_segments: int = 0,
                  bias_offsets=None, bias_tokens=None, bias_values=None, masks=None, row_mask=None):
         torch = _torch or _load_torch()
         self.tensors = (repetition, frequency, presence, temperature, bias_offsets, bias_tokens, bias_values, masks,
                         row_mask)
+        d = self.device = _device(self.tensors)
         per_row = [t for t in self.tensors[:4] + (row_mask,) if t is not None]
         self.rows = min((int(t.numel()) for t in per_row), default=None)
         biases = [t is not None for t in self.tensors[4:7]]
@@ -684,12 +712,12 @@ class LogitRules:
         self.counted = any(t is not None for t in self.tensors[:3])
         what = "penalties and temperature must be float32 [rows], contiguous"
         self.c = LogitRulesC(
-            *(_array(t, torch.float32, 0, what) for t in self.tensors[:4]), int(prompt_segments),
-            _array(bias_offsets, torch.int64, 1, "bias_offsets must be int64 [rows + 1], contiguous"),
-            _array(bias_tokens, torch.int32, 0, "bias_tokens must be int32, contiguous"),
-            _array(bias_values, torch.float32, nb, "bias_values must be float32, one per token, contiguous"), nb,
-            0 if masks is None else _array(masks, masks.dtype, 0, "masks must be contiguous"), nm, words,
-            _array(row_mask, torch.int32, 0, "row_mask must be int32 [rows], contiguous"))
+            *(_array(t, torch.float32, 0, what, d) for t in self.tensors[:4]), int(prompt_segments),
+            _array(bias_offsets, torch.int64, 1, "bias_offsets must be int64 [rows + 1], contiguous", d),
+            _array(bias_tokens, torch.int32, 0, "bias_tokens must be int32, contiguous", d),
+            _array(bias_values, torch.float32, nb, "bias_values must be float32, one per token, contiguous", d), nb,
+            0 if masks is None else _array(masks, masks.dtype, 0, "masks must be contiguous", d), nm, words,
+            _array(row_mask, torch.int32, 0, "row_mask must be int32 [rows], contiguous", d))
         self.ref = ctypes.byref(self.c)
 
 
@@ -704,7 +732,7 @@ def process_logits(logits, rules: LogitRules, graph: Optional[DeviceGraph] = Non
     if logits.dim() != 2 or logits.dtype not in (torch.float32, torch.bfloat16):
         raise ValueError("logits must be float32 or bfloat16 [rows, vocab]")
     rows, vocab = logits.shape
-    handle = _stream_handle(stream, logits) if logits.is_cuda else 0
+    handle, d = _stream_handle(stream, logits) if logits.is_cuda else 0, logits.get_device()
     if out is None:
         with _on(stream):
             out = torch.zeros((rows, vocab), dtype=torch.float32 if out_f32 else logits.dtype, device=logits.device)
@@ -720,10 +748,13 @@ def process_logits(logits, rules: LogitRules, graph: Optional[DeviceGraph] = Non
         raise ValueError("the values of a row must lie one behind the other")
     what = "row_branches and row_positions must be int32 [rows], contiguous"
     ids = _array(token_ids, torch.int32, 16 * graph.num_pages if graph is not None else 0,
-                 "token_ids must be int32, one per slot of the pool, contiguous")
-    bw, pw = _array(row_branches, torch.int32, rows, what), _array(row_positions, torch.int32, rows, what)
-    if not (logits.is_cuda and out.is_cuda):
-        raise ValueError("tensors passed to the library must live on the GPU")
+                 "token_ids must be int32, one per slot of the pool, contiguous", d)
+    bw, pw = _array(row_branches, torch.int32, rows, what, d), _array(row_positions, torch.int32, rows, what, d)
+    if d < 0 or d != out.get_device():
+        _elsewhere(min(d, out.get_device()), d)
+    for x in (rules, graph):
+        if x is not None and x.device is not None and x.device != d:
+            raise ValueError(f"the tensors of the rules or the graph live on device {x.device}, the logits on {d}")
     si, so = (t.stride(0) if rows > 1 else vocab for t in (logits, out))
     _check(lib.graphattn_process_logits(
         logits.data_ptr(), si, rows, vocab, GA_F32 if logits.dtype == torch.float32 else GA_BF16, rules.ref,
