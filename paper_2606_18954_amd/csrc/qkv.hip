@@ -55,12 +55,11 @@ struct Raw {
       for (int k = 0; k < 4; ++k) w[4 * i + k] = v[k];
     }
   }
-  __device__ __forceinline__ void store(unsigned char* p, bool past) const {
+  __device__ __forceinline__ void store(unsigned char* p) const {
 #pragma unroll
     for (int i = 0; i < W / 4; ++i) {
       const u32x4 v = {w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]};
-      if (past) __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(p) + i);
-      else reinterpret_cast<u32x4*>(p)[i] = v;
+      reinterpret_cast<u32x4*>(p)[i] = v;
     }
   }
   __device__ __forceinline__ void to(float (&x)[8]) const {
@@ -218,7 +217,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_qkv(QkvArgs a) {
     if constexpr (!FP4) {
       unsigned char* const page =
           a.pool + ((int64_t)(word >> 4) * a.Hkv * (2 * kPageTokens) + ((value ? kPageTokens : 0) + (word & 15))) * ROW;
-      if (h < a.Hkv) y.store(page + (unsigned)(h * (2 * kPageTokens * ROW) + c * SZ), a.past);
+      if (h < a.Hkv) y.store(page + (unsigned)(h * (2 * kPageTokens * ROW) + c * SZ));
     } else {
       unsigned code, byte;
       const unsigned w[4] = {y.w[0], y.w[1], y.w[2], y.w[3]};
@@ -253,7 +252,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_qkv(QkvArgs a) {
         if (i < n) {
           const int h = (i0 + i) * HPG + g;
           const Raw<T> y = made(r[i], t);
-          if (h < a.Hq) y.store(a.q_out + token * (a.Hq * ROW) + (unsigned)(h * ROW + c * SZ), a.past);
+          if (h < a.Hq) y.store(a.q_out + token * (a.Hq * ROW) + (unsigned)(h * ROW + c * SZ));
         }
     } else if (word >= 0 && (int64_t)word < a.num_slots) {
       const int i0 = (unit - a.q_units) * U::KV, n = min(U::KV, nk - i0);
@@ -296,9 +295,6 @@ hipError_t launch_qkv(const QkvArgs& args, int dim, int dtype, bool interleaved,
   const int kv = dtype == GA_F32 ? Units<float>::KV : Units<__bf16>::KV;
   a.q_units = (nq + q - 1) / q;
   a.q_groups = (nq + a.q_units - 1) / a.q_units;
-  // What is written goes past the caches where they could not hold it for the attention that follows (186 us, not 191,
-  // for the 940 MB above); a step's rows stay.
-  a.past = (int64_t)a.n * (a.Hq + 2 * a.Hkv) * dim * (dtype == GA_F32 ? 4 : 2) > (32 << 20);
   // Four tokens a workgroup where there are enough of them to fill the device (one: 207 us, two: 193, four: 192 before
   // the other steps), else one, its units on as many workgroups as they need.
   a.tokens = a.n >= 4096 ? kWaves : 1;

@@ -44,7 +44,6 @@ struct QkvArgs {
   int32_t n, Hq, Hkv, half;      // half: rotary_dim / 2
   int32_t q_units, q_groups;     // waves' shares of a token's queries, and groups of heads in each
   int32_t tokens;                // of a workgroup
-  bool past;                     // results past the caches
 };
 
 struct LogitArgs {
