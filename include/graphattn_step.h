@@ -151,7 +151,7 @@ typedef struct {
  * be NULL (row_branches and row_positions mark padding all the same).  A mask that forbids everything leaves a row
  * of -infinity.  GA_EUNSUPPORTED where rows x ceil(vocab / 38912) is 2^22 or more (with biases: vocab / 36864), and
  * for a vocab above 2^28.  Of a context the first 2^31 - 1 tokens
- * are seen, and a token's count is exact up to 2^30 - 1. */
+ * are seen; a token's count (below 2^30) is taken as a float32 value, exact up to 2^24. */
 ga_status graphattn_process_logits(const void* logits, int64_t logits_stride, int32_t rows,
                                    int32_t vocab, int32_t dtype, const ga_logit_rules* rules,
                                    const ga_device_graph* graph, const int32_t* token_ids,

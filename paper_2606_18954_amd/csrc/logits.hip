@@ -12,12 +12,13 @@
 // Biases: the flag says that there is one.  A list of up to 512 a row lies in LDS with the place of the first bias of
 // every 32 tokens; a longer one is searched in memory.
 //
-// Memory bounds it: 1024 rows of 152064 float32 values with penalties and biases, 1.25 GB in 238-254 us (a plain copy:
-// 234; without rules 238).  Eight waves per SIMD hide the counting (55 registers; at five 376 us): what is uniform and
-// rare, counts of 32 bits, has a loop of its own.  1024 rows of four drafted tokens a branch, 65024 bf16 values to
-// float32, contexts of some 14000 tokens: 96 us, where the same without penalties takes 63 and a copy 69: the
-// vector unit is busy two thirds of the time.  128 rows of 50001 with 300 biases and a mask each: 14 us, half of it the
-// chain from the branch to its tokens' counts; one row 6.2.
+// Memory bounds it: 1024 rows of 152064 float32 values with penalties and biases, 1.25 GB in 238-254 us (a plain
+// copy: 234; without rules 238).  Eight waves per SIMD hide the counting (55 vector registers, one of them with the
+// 52 scalar ones that do not fit; at five 376 us): what is uniform and rare, counts of 32 bits, has a loop of its
+// own.  1024 rows of four drafted tokens a branch, 65024 bf16 values to float32, contexts of 12200 tokens on average:
+// 96-109 us by the card, where the same without penalties takes 63 and a copy 69: the vector unit is busy two thirds
+// of the time.  128 rows of 50001 with 300 biases and a mask each: 14 us, half of it the chain from the branch to its
+// tokens' counts; one row 6.2.
 // (Rows of a branch in one workgroup that goes on with their counts: the drafts 115 us where they took 122, but the
 // 1024 rows 303 where they took 256.  Loads of 8 bytes where the output is twice as wide: 84 -> 63 us without rules.)
 #include <type_traits>
@@ -34,7 +35,7 @@ constexpr int kAhead = 2;          // fours of tokens of a thread whose loads ar
 constexpr int kBias = 512;         // biases of a row that LDS holds; a longer list is looked up in memory
 // Tokens of a slice, so that two workgroups share a CU's LDS: 76 KB of counts, or 72 and the biases.  (With half the
 // threads and slices, and four workgroups, every row's path is read twice as often: logits of 1024 rows of four drafted
-// tokens a branch over 65024 tokens, contexts of some 14000, take 117 us, not 99; 128 rows of 50001 15.6, not 14.6.)
+// tokens a branch over 65024 tokens, contexts of 12200, take 117 us, not 99; 128 rows of 50001 15.6, not 14.6.)
 constexpr int kMaxSlice = 38912, kMaxSliceBiased = 36864;
 
 typedef unsigned u32x4_any __attribute__((ext_vector_type(4), aligned(2)));

@@ -8,17 +8,17 @@
 //
 // 8 channels a lane, 16 bytes of bf16, so D / 8 lanes hold a head and a wave's load is a group of 512 / D heads.  A
 // workgroup takes one token, or four where there are many.  A token's rotary_dim / 2 angles are a wave's lanes', one
-// each (float64 product and remainder in turns, then sine and cosine of half turns in float32); they and the weights go
-// through LDS.  No table of angles is read, and positions may be any int32.  The groups are dealt to the waves in
-// units, three of q or one of k with the same heads of v, so that all loads of a unit go out before its first store:
-// a wave that waits for a load behind a store waits for the store too.
+// each (float64 product and remainder in turns, then sine and cosine of half turns in float32); they and the weights
+// go through LDS.  No table of angles is read, and positions go up to 2^31 - 1 (those below 0 are padding).  The
+// groups are dealt to the waves in units, three of q or one of k with the same heads of v, so that all loads of a
+// unit go out before its first store: a wave that waits for a load behind a store waits for the store too.
 //
 // Memory bounds it: 32768 tokens of 40 + 2 x 8 heads of 128, bf16, 940 MB in 170-187 us = 5.0-5.5 TB/s by the card (a
-// plain copy of as many bytes runs at 5.3), without norms or rotation the same; of 28 + 2 x 4 heads 105 us = 5.76 TB/s;
-// a step's 1024 tokens 5.5 us, one token 3.1 (replayed from a graph).  Counters: reads and writes are what the rows
-// hold, the vector unit is busy 37% of the time.  Before: one group after the other with a load ahead, angles exchanged
-// between lanes and made by every wave, 226 us and 20; five groups of q a unit 192 and 6.9 (more registers, five waves
-// per SIMD).
+// plain copy of as many bytes runs at 5.3), without norms or rotation the same; of 28 + 2 x 4 heads 105-119 us =
+// 5.1-5.8 TB/s; a step's 1024 tokens 5.5-6.3 us, one token 3.1 (replayed from a graph).  Counters: reads and writes
+// are what the rows hold, the vector unit is busy 37% of the time.  Before: one group after the other with a load
+// ahead, angles exchanged between lanes and made by every wave, 226 us and 20; five groups of q a unit 192 and 6.9
+// (more registers, five waves per SIMD).
 #include "mxfp4.hpp"
 #include "pool_load.hpp"
 #include "step_internal.hpp"
@@ -295,8 +295,11 @@ hipError_t launch_qkv(const QkvArgs& args, int dim, int dtype, bool interleaved,
   const int kv = dtype == GA_F32 ? Units<float>::KV : Units<__bf16>::KV;
   a.q_units = (nq + q - 1) / q;
   a.q_groups = (nq + a.q_units - 1) / a.q_units;
-  // Four tokens a workgroup where there are enough of them to fill the device (one: 207 us, two: 193, four: 192 before
-  // the other steps), else one, its units on as many workgroups as they need.
+  // Four tokens a workgroup where there are enough of them to fill the device, else one, its units on as many
+  // workgroups as they need.  One and four, us: 28 + 2 x 4 heads of 128, bf16, 1024 tokens 6.5 and 9.4, 2048 11.1 and
+  // 12.2, 3000 14.0 and 13.8, 4096 18.3 and 16.3, 8192 29.9 and 28.4, but 16384 58.5 and 61.5, 32768 110.5 and 118.2
+  // (40 + 2 x 8: 181 and 186); 12 + 2 x 12 of 64 2048 8.2 and 8.3, 4096 13.2 and 11.1, 16384 40.4 and 30.5; 16 + 2 x
+  // 2 of 64, float32, 2048 8.4 and 7.5, 16384 43.5 and 35.3.
   a.tokens = a.n >= 4096 ? kWaves : 1;
   const int units = a.q_units + (nk + kv - 1) / kv;
   const dim3 grid((unsigned)((a.n + a.tokens - 1) / a.tokens),

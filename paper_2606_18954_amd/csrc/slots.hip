@@ -310,8 +310,10 @@ dim3 tiles_of(int64_t items, int64_t capacity, int threads, int32_t* tile) {
   const int64_t splits = want < room ? want : room;
   return dim3((unsigned)tiles, (unsigned)(splits < 1 ? 1 : splits));
 }
-// From some thousand items on, the counts before a workgroup's are worth more threads (24,064 segments: 27 us with
-// 256, 21 with 1024 before the sums by row operations).
+// From some thousand items on, the counts before a workgroup's are worth more threads.  256 and 1024 threads, us:
+// tables of 1504 segments 5.1 and 7.0, 4089 6.1 and 7.4, 7050 7.0 and 8.0, 8930 8.9 and 8.5, 12032 10.8 and 8.8,
+// 24064 16.4 and 12.4; slots of 1024 branches 5.7 and 7.5, 6400 7.1 and 8.3, 11200 8.4 and 8.2, 24000 10.5 and 9.6,
+// 96000 36 and 22.
 int threads_of(int64_t items) { return items > 4096 ? 1024 : 256; }
 
 }  // namespace
