@@ -8,8 +8,8 @@ Tensors are contiguous and on one device.  The calls that take a pool check the 
 of the rows beside it and of slot words, lse and masses, and that each holds what the call reads or writes
 (about a microsecond a call); ValueError otherwise.  Without a stream a call goes to the current stream of
 the current device, and a pool (or mass) of another device is refused; the calls between two attention calls
-refuse tensors of two devices.  Outputs that a call makes itself are
-made on the stream that it goes to.
+refuse tensors of two devices.  Outputs that a call makes itself are made on the stream that it goes to: a program
+that uses them on another one orders that, and says so to the allocator (record_stream), as for any tensor.
 """
 from __future__ import annotations
 
